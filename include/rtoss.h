@@ -11,6 +11,9 @@
  *   rtoss_conv2d_pattern    convolution over the surviving weights only
  *                                                         (Section II.B cost model)
  *
+ * and, for the rest of a compressed model, products in 8-bit integers (rtoss_quantize_rows, rtoss_matmul_i8) and the gated
+ * feed-forward block with its backward pass (rtoss_gated_ff, rtoss_gated_ff_i8, rtoss_gated_ff_backward),
+ *
  * plus the host-side dictionary generator rtoss_pattern_dict (Section IV.B, Eq. 1 and the
  * adjacency criterion) and the usage-based dictionary reduction of the same section
  * (rtoss_pattern_histogram on the device, rtoss_reduce_dict on the host).
@@ -340,6 +343,97 @@ rtoss_status rtoss_conv2d_pattern_coherent(const rtoss_wdesc* desc, const rtoss_
                                            const uint16_t* masks_host, int P,
                                            const void* packed_dev, const void* x_dev, void* y_dev,
                                            void* hip_stream);
+
+/*
+ * Products in 8-bit integers and the gated feed-forward block: what stands next to the pruned 1x1 layers in a
+ * compressed model.  Their rows are tokens or positions (a channels-last tensor's positions, as for 1x1 layers), their
+ * weights [channels out][channels in] matrices.
+ *
+ * Common to the calls below
+ *   - A pitch (x_ld, a_ld, w_ld, h_ld, q_ld) is the number of elements from one row's first to the next row's; 0 means a
+ *     plain matrix.  A larger one makes the matrix a slice of a wider buffer (two weight matrices stored in one, the
+ *     channels of a concatenation); what lies between the rows is neither read nor written.  Pointers and pitches need
+ *     only the alignment of their elements; rows of whole 16-byte pieces that start at multiples of 16 bytes are the fast path.
+ *   - Rows 0 <= M < 2^31 (M = 0: nothing to do, row pointers may be NULL), channels 1 .. 2^24, pitches below 2^31 elements.
+ *   - Results may not overlap operands or each other (checked for plain matrices).
+ *   - Determinism: as above; no atomics, one order of additions for a shape, a type and the operands' alignment.
+ */
+
+/*
+ * Rows to signed 8-bit codes with one scale each (the tokens of an activation tensor; the output channels of a weight
+ * matrix):
+ *     scale[m] = max_k |x[m][k]| / 127 (rounded to fp32),   q[m][k] = nearest integer to x[m][k] * 127 / max, ties to even
+ * The code is that of the exact quotient.  A row of zeros has scale 0 and codes 0; a row that holds an infinity or a NaN
+ * has scale NaN and codes 0, so that what is computed from it is NaN.
+ *
+ *   x_dev      M x K values of type dt, pitch x_ld          q_dev      out: M x K codes in -127 .. 127, pitch q_ld
+ *   scale_dev  out: M floats
+ * Errors: RTOSS_EDTYPE, RTOSS_ESHAPE, RTOSS_EINVAL.
+ */
+rtoss_status rtoss_quantize_rows(const void* x_dev, rtoss_dtype dt, int64_t M, int64_t K, int64_t x_ld,
+                                 int8_t* q_dev, int64_t q_ld, float* scale_dev, void* hip_stream);
+
+/* One product in 8-bit integers. */
+typedef struct {
+    int64_t M;           /* rows */
+    int N, K;            /* channels out and in; K < 2^17, so that no sum passes 32 bits */
+    int64_t a_ld, w_ld;  /* pitches */
+    rtoss_dtype out_dt;  /* any */
+} rtoss_matmul_desc;
+
+/*
+ *     y[m][n] = act(a_scale[m] * scale[n] * sum_k a[m][k] * w[n][k] + bias[n]) + residual[m][n]
+ * The sum is exact (32-bit integers); the rest is fp32, rounded once on store.
+ *
+ *   a_dev, a_scale_dev  M x K codes (any of -128 .. 127) and M scales, or NULL for scales of 1
+ *   w_dev               N x K codes; their scales are the epilogue's scale_dev
+ *   epilogue            as for rtoss_conv2d_pattern_fused with N for Co, or NULL for none; here its vectors need 4-byte, y and the
+ *                       residual only their element's alignment
+ * Errors: RTOSS_EDTYPE, RTOSS_ESHAPE, RTOSS_EINVAL.
+ */
+rtoss_status rtoss_matmul_i8(const rtoss_matmul_desc* desc, const int8_t* a_dev, const float* a_scale_dev,
+                             const int8_t* w_dev, const rtoss_epilogue* epilogue, void* y_dev, void* hip_stream);
+
+/* One gated feed-forward block: x [M][K], w_gate and w_up [F][K], h [M][F]. */
+typedef struct {
+    int64_t M;
+    int K, F;
+    rtoss_dtype dt;             /* of all tensors; with 8-bit operands, of h */
+    rtoss_act act;              /* of the gate */
+    int64_t x_ld, w_ld, h_ld;   /* pitches: of x, of both weights, of h (and its gradient) */
+} rtoss_gated_desc;
+
+/*
+ *     g = x w_gate^T,   u = x w_up^T,   h = act(g) * u
+ * Sums in fp32; h is rounded once.
+ *   gate_dev, up_dev  out: g and u, plain [M][F], rounded once each, for rtoss_gated_ff_backward; or both NULL (nothing is kept)
+ * Errors: RTOSS_EDTYPE, RTOSS_ESHAPE, RTOSS_EINVAL.
+ */
+rtoss_status rtoss_gated_ff(const rtoss_gated_desc* desc, const void* x_dev, const void* w_gate_dev, const void* w_up_dev,
+                            void* h_dev, void* gate_dev, void* up_dev, void* hip_stream);
+
+/* The same on codes with scales (K < 2^17): g[m][f] = a_scale[m] * gate_scale[f] * sum, u likewise; scales may be NULL for 1. */
+rtoss_status rtoss_gated_ff_i8(const rtoss_gated_desc* desc, const int8_t* a_dev, const float* a_scale_dev,
+                               const int8_t* w_gate_dev, const float* gate_scale_dev,
+                               const int8_t* w_up_dev, const float* up_scale_dev, void* h_dev, void* hip_stream);
+
+/*
+ * Gradients of rtoss_gated_ff from that of h:
+ *     dg = dh * u * act'(g),  du = dh * act(g)     (in fp32, then rounded to dt; act' of ReLU at 0 is 0)
+ *     dx = dg w_gate + du w_up,   dw_gate = dg^T x,   dw_up = du^T x     (sums in fp32, rounded once)
+ *
+ *   dh_dev                  M x F, pitch h_ld          gate_dev, up_dev  as rtoss_gated_ff kept them
+ *   dx_dev                  out: plain [M][K], or NULL (not computed; the weights may then be NULL)
+ *   dw_gate_dev, dw_up_dev  out: plain [F][K], or both NULL (x may then be NULL).  Of no rows (M = 0) they are zero.
+ *   workspace_dev           scratch of the size that rtoss_gated_ff_backward_size gives for the descriptor (host only, no GPU
+ *                           needed), 256-byte aligned; it holds nothing between calls
+ * Errors: RTOSS_EDTYPE, RTOSS_ESHAPE, RTOSS_EINVAL, RTOSS_ENOSPACE.
+ */
+rtoss_status rtoss_gated_ff_backward_size(const rtoss_gated_desc* desc, size_t* workspace_bytes);
+rtoss_status rtoss_gated_ff_backward(const rtoss_gated_desc* desc, const void* dh_dev, const void* x_dev,
+                                     const void* w_gate_dev, const void* w_up_dev, const void* gate_dev, const void* up_dev,
+                                     void* dx_dev, void* dw_gate_dev, void* dw_up_dev,
+                                     void* workspace_dev, size_t workspace_bytes, void* hip_stream);
 
 /* Message for the last error on the calling thread ("" if none).  Static storage. */
 const char* rtoss_last_error(void);

@@ -45,6 +45,16 @@ class EpilogueDesc(ctypes.Structure):
                 ("residual_dev", ctypes.c_void_p), ("y_ld", ctypes.c_int), ("residual_ld", ctypes.c_int)]
 
 
+class MatmulDesc(ctypes.Structure):
+    _fields_ = [("M", ctypes.c_int64), ("N", ctypes.c_int), ("K", ctypes.c_int), ("a_ld", ctypes.c_int64), ("w_ld", ctypes.c_int64),
+                ("out_dt", ctypes.c_int)]
+
+
+class GatedDesc(ctypes.Structure):
+    _fields_ = [("M", ctypes.c_int64), ("K", ctypes.c_int), ("F", ctypes.c_int), ("dt", ctypes.c_int), ("act", ctypes.c_int),
+                ("x_ld", ctypes.c_int64), ("w_ld", ctypes.c_int64), ("h_ld", ctypes.c_int64)]
+
+
 class PackItemDesc(ctypes.Structure):
     _fields_ = [("desc", WDesc), ("w_dev", ctypes.c_void_p), ("idx_dev", ctypes.c_void_p), ("packed_dev", ctypes.c_void_p),
                 ("packed_bytes", ctypes.c_size_t)]
@@ -56,7 +66,9 @@ class SelectItem(ctypes.Structure):
 
 EXPORTS = ["rtoss_pattern_dict", "rtoss_select_patterns", "rtoss_select_patterns_batch", "rtoss_pattern_histogram", "rtoss_reduce_dict",
            "rtoss_pack_size", "rtoss_pack", "rtoss_pack_batch", "rtoss_conv2d_pattern", "rtoss_conv2d_pattern_fused",
-           "rtoss_pack_size_coherent", "rtoss_pack_coherent", "rtoss_conv2d_pattern_coherent", "rtoss_last_error"]
+           "rtoss_pack_size_coherent", "rtoss_pack_coherent", "rtoss_conv2d_pattern_coherent", "rtoss_quantize_rows",
+           "rtoss_matmul_i8", "rtoss_gated_ff", "rtoss_gated_ff_i8", "rtoss_gated_ff_backward_size", "rtoss_gated_ff_backward",
+           "rtoss_last_error"]
 
 
 def lib():
@@ -103,6 +115,18 @@ def lib():
         L.rtoss_conv2d_pattern_coherent.restype = i
         L.rtoss_conv2d_pattern_coherent.argtypes = [ctypes.POINTER(WDesc), ctypes.POINTER(CDesc), ctypes.POINTER(EpilogueDesc),
                                                     u16p, i, vp, vp, vp, vp]
+        L.rtoss_quantize_rows.restype = i
+        L.rtoss_quantize_rows.argtypes = [vp, i, i64, i64, i64, vp, i64, vp, vp]
+        L.rtoss_matmul_i8.restype = i
+        L.rtoss_matmul_i8.argtypes = [ctypes.POINTER(MatmulDesc), vp, vp, vp, ctypes.POINTER(EpilogueDesc), vp, vp]
+        L.rtoss_gated_ff.restype = i
+        L.rtoss_gated_ff.argtypes = [ctypes.POINTER(GatedDesc)] + [vp] * 7
+        L.rtoss_gated_ff_i8.restype = i
+        L.rtoss_gated_ff_i8.argtypes = [ctypes.POINTER(GatedDesc)] + [vp] * 8
+        L.rtoss_gated_ff_backward_size.restype = i
+        L.rtoss_gated_ff_backward_size.argtypes = [ctypes.POINTER(GatedDesc), szp]
+        L.rtoss_gated_ff_backward.restype = i
+        L.rtoss_gated_ff_backward.argtypes = [ctypes.POINTER(GatedDesc)] + [vp] * 10 + [ctypes.c_size_t, vp]
         _lib = L
     return _lib
 
@@ -252,3 +276,36 @@ def rtoss_pack_batch(items, masks, stream=0):
         arr[i] = PackItemDesc(wd, w_ptr, idx_ptr, packed_ptr, int(packed_bytes))
     _check(lib().rtoss_pack_batch(arr, len(items), mp, P, stream))
 
+
+def _ref(desc):
+    return ctypes.byref(desc) if desc is not None else None
+
+
+def rtoss_quantize_rows(x_ptr, dt, M, K, q_ptr, scale_ptr, x_ld=0, q_ld=0, stream=0):
+    _check(lib().rtoss_quantize_rows(x_ptr, int(dt), int(M), int(K), int(x_ld), q_ptr, int(q_ld), scale_ptr, stream))
+
+
+def rtoss_matmul_i8(desc, a_ptr, a_scale_ptr, w_ptr, epilogue, y_ptr, stream=0):
+    """desc: MatmulDesc; epilogue: EpilogueDesc (channel scales, bias, activation, residual) or None."""
+    _check(lib().rtoss_matmul_i8(_ref(desc), a_ptr, a_scale_ptr, w_ptr, _ref(epilogue), y_ptr, stream))
+
+
+def rtoss_gated_ff(desc, x_ptr, w_gate_ptr, w_up_ptr, h_ptr, gate_ptr=None, up_ptr=None, stream=0):
+    """desc: GatedDesc."""
+    _check(lib().rtoss_gated_ff(_ref(desc), x_ptr, w_gate_ptr, w_up_ptr, h_ptr, gate_ptr, up_ptr, stream))
+
+
+def rtoss_gated_ff_i8(desc, a_ptr, a_scale_ptr, w_gate_ptr, gate_scale_ptr, w_up_ptr, up_scale_ptr, h_ptr, stream=0):
+    _check(lib().rtoss_gated_ff_i8(_ref(desc), a_ptr, a_scale_ptr, w_gate_ptr, gate_scale_ptr, w_up_ptr, up_scale_ptr, h_ptr, stream))
+
+
+def rtoss_gated_ff_backward_size(desc):
+    n = ctypes.c_size_t(0)
+    _check(lib().rtoss_gated_ff_backward_size(_ref(desc), ctypes.byref(n)))
+    return n.value
+
+
+def rtoss_gated_ff_backward(desc, dh_ptr, x_ptr, w_gate_ptr, w_up_ptr, gate_ptr, up_ptr, dx_ptr, dw_gate_ptr, dw_up_ptr, workspace_ptr,
+                            workspace_bytes, stream=0):
+    _check(lib().rtoss_gated_ff_backward(_ref(desc), dh_ptr, x_ptr, w_gate_ptr, w_up_ptr, gate_ptr, up_ptr, dx_ptr, dw_gate_ptr,
+                                         dw_up_ptr, workspace_ptr, workspace_bytes, stream))

@@ -7,10 +7,13 @@
 #include <Python.h>
 
 #include <ATen/hip/EmptyTensor.h>
+#include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <algorithm>
 #include <cstring>
+#include <initializer_list>
 #include <memory>
 #include <string>
 #include <vector>
@@ -447,6 +450,272 @@ PyObject* py_histogram(PyObject*, PyObject* const* a, Py_ssize_t n)
     });
 }
 
+// ---- 8-bit products and the gated block ----
+int dtype_of(const at::Tensor& t)
+{
+    switch (t.scalar_type()) {
+    case at::kFloat: return RTOSS_F32;
+    case at::kHalf: return RTOSS_F16;
+    case at::kBFloat16: return RTOSS_BF16;
+    default: raise(PyExc_TypeError, "float32, float16 or bfloat16 tensors are expected");
+    }
+}
+// A tensor as rows of its last dimension: the others collapse to one with a constant pitch.
+struct Rows {
+    int64_t M, K, ld;
+};
+Rows rows_of(const at::Tensor& t)
+{
+    const auto z = t.sizes(), st = t.strides();
+    const int64_t n = t.dim();
+    require(n >= 1, "a tensor of rows has at least 1 dimension");
+    Rows r{1, z[n - 1], z[n - 1]};
+    bool found = false;
+    int64_t next = 0;  // stride that the next outer dimension has to have
+    for (int64_t i = n - 2; i >= 0; --i) r.M *= z[i];
+    if (r.M == 0 || r.K == 0) return r;
+    require(r.K == 1 || st[n - 1] == 1, "the elements of a row must be contiguous");
+    for (int64_t i = n - 2; i >= 0; --i) {
+        if (z[i] == 1) continue;
+        if (!found) r.ld = st[i], found = true;
+        else require(st[i] == next, "the rows of a tensor must lie at one distance from each other");
+        next = st[i] * z[i];
+    }
+    require(r.ld >= r.K, "the rows of a tensor must not overlap");
+    return r;
+}
+// What a call's tensors have in common: the GPU they are on.  Kernels run there, on its current stream.
+struct OnDevice {
+    at::Device dev;
+    c10::DeviceGuard guard;
+    void* stream;
+    explicit OnDevice(const at::Tensor& t)
+        : dev((require(t.is_cuda(), "tensors must be on the GPU"), t.device())), guard(dev), stream((void*)c10::hip::getCurrentHIPStream(dev.index()).stream())
+    {
+    }
+    const at::Tensor& here(const at::Tensor& t) const
+    {
+        require(t.is_cuda() && t.device() == dev, "all tensors of a call must be on one GPU");
+        return t;
+    }
+    const at::Tensor& here(PyObject* o) const { return here(tensor(o)); }
+};
+void require_type(const at::Tensor& t, at::ScalarType st, const char* msg) { require(t.scalar_type() == st, msg); }
+int extent(int64_t v)  // (a size past the library's range is the library's error to report)
+{
+    return (int)std::min<int64_t>(v, 0x7fffffff);
+}
+const float* scales_arg(PyObject* o, int64_t n, const OnDevice& on)
+{
+    if (o == Py_None) return nullptr;
+    const at::Tensor& t = on.here(o);
+    require(t.scalar_type() == at::kFloat && t.is_contiguous() && t.numel() == n,
+            "scales and bias are contiguous float32 tensors with one element per row or channel");
+    return (const float*)t.data_ptr();
+}
+std::vector<int64_t> with_last(const at::Tensor& x, int64_t last)
+{
+    std::vector<int64_t> shape = x.sizes().vec();
+    shape.back() = last;
+    return shape;
+}
+// a result: allocated, or the caller's, of a given shape and type
+struct Result {
+    at::Tensor t;
+    PyObject* given = nullptr;
+    PyObject* wrap()
+    {
+        if (!given) return THPVariable_Wrap(std::move(t));
+        Py_INCREF(given);
+        return given;
+    }
+};
+Result result_arg(PyObject* o, const std::vector<int64_t>& shape, at::ScalarType st, const OnDevice& on)
+{
+    if (o == Py_None) return Result{allocate(shape, st, on.dev)};
+    const at::Tensor& t = on.here(o);
+    require(t.sizes() == at::IntArrayRef(shape) && t.scalar_type() == st, "a result has the wrong shape or dtype");
+    return Result{t, o};
+}
+PyObject* tuple_of(std::initializer_list<PyObject*> items)
+{
+    Owned out(PyTuple_New((Py_ssize_t)items.size()));
+    Py_ssize_t i = 0;
+    bool ok = true;
+    for (PyObject* o : items) {
+        ok &= o != nullptr;
+        PyTuple_SET_ITEM(out.o, i++, o);
+    }
+    if (!ok) throw PyError{};
+    return out.release();
+}
+
+// quantize_rows(x, q or None, scale or None) -> (q, scale)
+PyObject* py_quantize_rows(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject* {
+        arity(n, 3);
+        const at::Tensor& x = tensor(a[0]);
+        const OnDevice on(x);
+        const int dt = dtype_of(x);
+        const Rows r = rows_of(x);
+        Result q = result_arg(a[1], x.sizes().vec(), at::kChar, on);
+        std::vector<int64_t> outer = x.sizes().vec();
+        outer.pop_back();
+        Result scale = result_arg(a[2], outer, at::kFloat, on);
+        require(scale.t.is_contiguous(), "scale must be contiguous");
+        const Rows rq = rows_of(q.t);
+        const void* xp = x.data_ptr();
+        auto* qp = (int8_t*)q.t.data_ptr();
+        auto* sp = (float*)scale.t.data_ptr();
+        call([&] { return rtoss_quantize_rows(xp, (rtoss_dtype)dt, r.M, r.K, r.ld, qp, rq.ld, sp, on.stream); });
+        return tuple_of({q.wrap(), scale.wrap()});
+    });
+}
+
+// matmul_i8(a, a_scale, w, w_scale, bias, act, residual, out_dt, y) -> y
+PyObject* py_matmul_i8(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject* {
+        arity(n, 9);
+        const at::Tensor& x = tensor(a[0]);
+        const OnDevice on(x);
+        const at::Tensor& w = on.here(a[2]);
+        require_type(x, at::kChar, "a and w are int8 tensors");
+        require_type(w, at::kChar, "a and w are int8 tensors");
+        require(w.dim() == 2, "w is a matrix [N, K]");
+        const Rows r = rows_of(x), rw = rows_of(w);
+        require(r.K == rw.K, "a has another number of channels than w");
+        const int out_dt = (int)integer(a[7]);
+        Result y = result_arg(a[8], with_last(x, rw.M), scalar_type(out_dt), on);
+        rtoss_epilogue e{};
+        const float* sa = scales_arg(a[1], r.M, on);
+        e.scale_dev = scales_arg(a[3], rw.M, on);
+        e.bias_dev = scales_arg(a[4], rw.M, on);
+        e.act = (rtoss_act)integer(a[5]);
+        e.y_ld = extent(rows_of(y.t).ld);
+        if (a[6] != Py_None) {
+            const at::Tensor& res = on.here(a[6]);
+            require(res.sizes() == y.t.sizes() && res.scalar_type() == y.t.scalar_type(), "residual must have y's shape and dtype");
+            e.residual_dev = res.data_ptr();
+            e.residual_ld = extent(rows_of(res).ld);
+        }
+        const rtoss_matmul_desc d{r.M, extent(rw.M), extent(r.K), r.ld, rw.ld, (rtoss_dtype)out_dt};
+        const auto *xp = (const int8_t*)x.data_ptr(), *wp = (const int8_t*)w.data_ptr();
+        void* yp = y.t.data_ptr();
+        call([&] { return rtoss_matmul_i8(&d, xp, sa, wp, &e, yp, on.stream); });
+        return y.wrap();
+    });
+}
+
+// the weights of a gated block: two matrices of one shape, type and pitch
+struct GatedWeights {
+    Rows r;
+    const void *gate, *up;
+};
+GatedWeights gated_weights(const at::Tensor& g, const at::Tensor& u, at::ScalarType st, int64_t K)
+{
+    require(g.dim() == 2 && g.sizes() == u.sizes() && g.scalar_type() == st && u.scalar_type() == st,
+            "w_gate and w_up are matrices [F, K] of one shape, and of x's dtype");
+    const Rows r = rows_of(g), ru = rows_of(u);
+    require(r.K == K, "x has another number of channels than the weights");
+    require(r.ld == ru.ld || r.M <= 1, "w_gate and w_up must have the same pitch");
+    return GatedWeights{r, g.data_ptr(), u.data_ptr()};
+}
+
+// gated_ff(x, w_gate, w_up, act, keep, h) -> h, or (h, gate, up)
+PyObject* py_gated_ff(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject* {
+        arity(n, 6);
+        const at::Tensor& x = tensor(a[0]);
+        const OnDevice on(x);
+        const int dt = dtype_of(x);
+        const Rows r = rows_of(x);
+        const GatedWeights w = gated_weights(on.here(a[1]), on.here(a[2]), x.scalar_type(), r.K);
+        const int act = (int)integer(a[3]);
+        const bool keep = truth(a[4]);
+        const auto shape = with_last(x, w.r.M);
+        Result h = result_arg(a[5], shape, x.scalar_type(), on);
+        at::Tensor gate, up;
+        if (keep) {
+            gate = allocate(shape, x.scalar_type(), on.dev);
+            up = allocate(shape, x.scalar_type(), on.dev);
+        }
+        const rtoss_gated_desc d{r.M, extent(r.K), extent(w.r.M), (rtoss_dtype)dt, (rtoss_act)act, r.ld, w.r.ld, rows_of(h.t).ld};
+        const void* xp = x.data_ptr();
+        void *hp = h.t.data_ptr(), *gp = keep ? gate.data_ptr() : nullptr, *up_p = keep ? up.data_ptr() : nullptr;
+        call([&] { return rtoss_gated_ff(&d, xp, w.gate, w.up, hp, gp, up_p, on.stream); });
+        if (!keep) return h.wrap();
+        return tuple_of({h.wrap(), THPVariable_Wrap(std::move(gate)), THPVariable_Wrap(std::move(up))});
+    });
+}
+
+// gated_ff_i8(a, a_scale, w_gate, gate_scale, w_up, up_scale, act, out_dt, h) -> h
+PyObject* py_gated_ff_i8(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject* {
+        arity(n, 9);
+        const at::Tensor& x = tensor(a[0]);
+        const OnDevice on(x);
+        require_type(x, at::kChar, "a, w_gate and w_up are int8 tensors");
+        const Rows r = rows_of(x);
+        const GatedWeights w = gated_weights(on.here(a[2]), on.here(a[4]), at::kChar, r.K);
+        const float *sa = scales_arg(a[1], r.M, on), *sg = scales_arg(a[3], w.r.M, on), *su = scales_arg(a[5], w.r.M, on);
+        const int act = (int)integer(a[6]), out_dt = (int)integer(a[7]);
+        Result h = result_arg(a[8], with_last(x, w.r.M), scalar_type(out_dt), on);
+        const rtoss_gated_desc d{r.M, extent(r.K), extent(w.r.M), (rtoss_dtype)out_dt, (rtoss_act)act, r.ld, w.r.ld, rows_of(h.t).ld};
+        const auto* xp = (const int8_t*)x.data_ptr();
+        void* hp = h.t.data_ptr();
+        call([&] { return rtoss_gated_ff_i8(&d, xp, sa, (const int8_t*)w.gate, sg, (const int8_t*)w.up, su, hp, on.stream); });
+        return h.wrap();
+    });
+}
+
+// gated_ff_backward(dh, x, w_gate, w_up, gate, up, act, rows, weights, workspace or None) -> (dx or None, dw_gate or None, dw_up or None)
+PyObject* py_gated_ff_backward(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject* {
+        arity(n, 10);
+        const at::Tensor &dh = tensor(a[0]), &x = tensor(a[1]);
+        const OnDevice on(x);
+        const int dt = dtype_of(x);
+        const Rows r = rows_of(x);
+        const GatedWeights w = gated_weights(on.here(a[2]), on.here(a[3]), x.scalar_type(), r.K);
+        const at::Tensor &gate = on.here(a[4]), &up = on.here(a[5]);
+        const auto shape = with_last(x, w.r.M);
+        on.here(dh);
+        for (const at::Tensor* t : {&dh, &gate, &up})
+            require(t->sizes() == at::IntArrayRef(shape) && t->scalar_type() == x.scalar_type(), "dh, gate and up must have h's shape and dtype");
+        require(gate.is_contiguous() && up.is_contiguous(), "gate and up must be contiguous");
+        const int act = (int)integer(a[6]);
+        const bool rows = truth(a[7]), weights = truth(a[8]);
+        const rtoss_gated_desc d{r.M, extent(r.K), extent(w.r.M), (rtoss_dtype)dt, (rtoss_act)act, r.ld, w.r.ld, rows_of(dh).ld};
+        size_t bytes = 0;
+        check(rtoss_gated_ff_backward_size(&d, &bytes));
+        at::Tensor made;
+        if (a[9] == Py_None) made = allocate({(int64_t)bytes}, at::kByte, on.dev);
+        const at::Tensor& workspace = a[9] == Py_None ? made : on.here(a[9]);
+        require(workspace.scalar_type() == at::kByte && workspace.is_contiguous(), "workspace must be a contiguous uint8 tensor");
+        at::Tensor dx, dg, du;
+        if (rows) dx = allocate(x.sizes(), x.scalar_type(), on.dev);
+        if (weights) {
+            dg = allocate({w.r.M, w.r.K}, x.scalar_type(), on.dev);
+            du = allocate({w.r.M, w.r.K}, x.scalar_type(), on.dev);
+        }
+        const void *hp = dh.data_ptr(), *xp = x.data_ptr(), *gp = gate.data_ptr(), *up_p = up.data_ptr();
+        void *dxp = rows ? dx.data_ptr() : nullptr, *dgp = weights ? dg.data_ptr() : nullptr, *dup = weights ? du.data_ptr() : nullptr;
+        void* wsp = workspace.data_ptr();
+        const size_t have = (size_t)workspace.numel();
+        call([&] { return rtoss_gated_ff_backward(&d, hp, xp, w.gate, w.up, gp, up_p, dxp, dgp, dup, wsp, have, on.stream); });
+        auto wrap = [](at::Tensor& t, bool there) -> PyObject* {
+            if (there) return THPVariable_Wrap(std::move(t));
+            Py_RETURN_NONE;
+        };
+        return tuple_of({wrap(dx, rows), wrap(dg, weights), wrap(du, weights)});
+    });
+}
+
 // set_error_type(RtossError)
 PyObject* py_set_error_type(PyObject*, PyObject* type)
 {
@@ -457,6 +726,7 @@ PyObject* py_set_error_type(PyObject*, PyObject* type)
 
 #define FAST(name) {#name, (PyCFunction)(void (*)(void))py_##name, METH_FASTCALL, nullptr}
 PyMethodDef kMethods[] = {FAST(layer), FAST(conv), FAST(conv_fused), FAST(select), FAST(select_batch), FAST(pack_batch), FAST(histogram),
+                          FAST(quantize_rows), FAST(matmul_i8), FAST(gated_ff), FAST(gated_ff_i8), FAST(gated_ff_backward),
                           {"set_error_type", py_set_error_type, METH_O, nullptr},
                           {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_host", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};

@@ -68,6 +68,37 @@ def reduce_dictionary(masks, w_random, dt, M):
     return out, kept, counts
 
 
+# Rows are the positions (tokens) of a tensor whose last dimension is the channels; they may lie in a wider buffer.  Results are allocated
+# unless they are given.  Calls run on the tensors' GPU, on its current stream.
+def quantize_rows(x, q=None, scale=None):
+    """Signed 8-bit codes and a scale for each row of x [..., K] (float32, float16 or bfloat16): activations by token, weights [N, K] by
+    output channel.  Returns (q [..., K] int8, scale [...] float32)."""
+    return B.host().quantize_rows(x, q, scale)
+
+
+def matmul_i8(a, a_scale, w, w_scale, bias=None, act=B.ACT_NONE, residual=None, out_dt=B.BF16, y=None):
+    """y = act(a_scale[row] * w_scale[n] * (a w^T) + bias[n]) + residual.  a: int8 rows [..., K]; w: int8 [N, K]; scales and bias: float32 or
+    None; residual: of y's shape and dtype or None.  Returns y [..., N] of out_dt."""
+    return B.host().matmul_i8(a, a_scale, w, w_scale, bias, act, residual, out_dt, y)
+
+
+def gated_ff(x, w_gate, w_up, act=B.ACT_SILU, keep=False, h=None):
+    """h = act(x w_gate^T) * (x w_up^T).  x: rows [..., K]; weights [F, K] of x's dtype.  Returns h [..., F]; with keep, (h, gate, up): the two
+    projections, which gated_ff_backward takes."""
+    return B.host().gated_ff(x, w_gate, w_up, act, keep, h)
+
+
+def gated_ff_i8(a, a_scale, w_gate, gate_scale, w_up, up_scale, act=B.ACT_SILU, out_dt=B.BF16, h=None):
+    """gated_ff on 8-bit rows and weights with their scales (quantize_rows).  Returns h [..., F] of out_dt."""
+    return B.host().gated_ff_i8(a, a_scale, w_gate, gate_scale, w_up, up_scale, act, out_dt, h)
+
+
+def gated_ff_backward(dh, x, w_gate, w_up, gate, up, act=B.ACT_SILU, rows=True, weights=True, workspace=None):
+    """Gradients of gated_ff from that of its result: (dx, dw_gate, dw_up), None for those that are not asked for (rows: dx; weights: the
+    other two).  workspace: a uint8 tensor of B.rtoss_gated_ff_backward_size bytes, or None."""
+    return B.host().gated_ff_backward(dh, x, w_gate, w_up, gate, up, act, rows, weights, workspace)
+
+
 class _Layer:
     """What both kinds of layer share: the native handle through which calls read the descriptor (wdesc) and the
     dictionary (masks).  It reads them where the attributes keep them, follows an attribute that is replaced, and is made

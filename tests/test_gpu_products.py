@@ -1,0 +1,563 @@
+"""The 8-bit products and the gated feed-forward block against plain implementations in 64 bits.
+
+Two kinds of inputs.  Small whole numbers: every product and sum is exact in fp32, so results must equal the rounded reference bit for bit,
+whatever the order of the additions; this checks indexes, tails, pitches and masks of every kernel.  Normal values: compared within the
+roundings of the formula, counted as half a step, 2^-24 of the value in fp32, for each operation and each addition of a sum."""
+import pytest
+import torch
+
+from paper_2303_02191_amd import binding as B
+from paper_2303_02191_amd import pipeline as pl
+
+pytestmark = pytest.mark.gpu
+
+DT = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+ABI = {"f32": B.F32, "f16": B.F16, "bf16": B.BF16}
+U = 2.0 ** -24
+
+
+def gen(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return g
+
+
+def whole(g, shape, top, dt=torch.float32):
+    return torch.randint(-top, top + 1, shape, generator=g, device="cuda").to(dt)
+
+
+def normal(g, shape, std=1.0):
+    return torch.randn(shape, generator=g, device="cuda") * std
+
+
+def codes(g, shape):
+    return torch.randint(-128, 128, shape, generator=g, device="cuda").to(torch.int8)
+
+
+def inside(t, pitch, fill):
+    """t as a slice of a wider buffer whose other elements are `fill`: (view, buffer).  The first element is no multiple of 16 bytes either."""
+    if not pitch:
+        return t.contiguous(), None
+    buf = torch.full((t.shape[0], t.shape[1] + pitch), fill, dtype=t.dtype, device=t.device)
+    view = buf[:, pitch // 2: pitch // 2 + t.shape[1]]
+    view.copy_(t)
+    return view, buf
+
+
+def act(v, a):
+    return v if a == 0 else torch.relu(v) if a == 1 else v * torch.sigmoid(v)
+
+
+def half_step(dt):
+    return torch.finfo(dt).eps / 2
+
+
+def least(dt):
+    return torch.finfo(dt).smallest_normal * torch.finfo(dt).eps / 2  # half a step among the subnormal numbers
+
+
+def check(got, want, tol, what=""):
+    d = (got.double() - want).abs()
+    bad = ~(d <= tol)
+    assert not bad.any(), "%s: %d of %d off, first at %s: got %r, want %r, allowed %r" % (
+        what, int(bad.sum()), bad.numel(), bad.nonzero()[0].tolist(), got[bad][0].item(), want[bad][0].item(), tol[bad][0].item())
+
+
+def equal(got, want, what=""):
+    same = got == want
+    assert same.all(), "%s: %d of %d differ, first at %s: got %r, want %r" % (
+        what, int((~same).sum()), same.numel(), (~same).nonzero()[0].tolist(), got[~same][0].item(), want[~same][0].item())
+
+
+# (M, K, N): one of everything, tails below and behind a tile and a stage, whole tiles, few rows of long sums, several tiles
+SHAPES = [(1, 1, 1), (1, 64, 16), (1, 1000, 40), (2, 4096, 256), (3, 17, 5), (7, 256, 100), (16, 512, 64), (17, 31, 65), (33, 1024, 96),
+          (64, 64, 64), (65, 130, 33), (77, 1021, 203), (128, 384, 128), (129, 72, 257), (200, 256, 192), (257, 100, 515), (300, 520, 387),
+          (513, 1152, 640), (1030, 192, 300)]
+
+
+# ---------------------------------------------------------------------------------------------------------
+# rows to codes
+# ---------------------------------------------------------------------------------------------------------
+def quantized(x):
+    v = x.double()
+    top = v.abs().amax(-1, keepdim=True)
+    q = torch.where(top > 0, v * 127 / top, torch.zeros_like(v))
+    return q.round().to(torch.int8), (top / 127).squeeze(-1).float()
+
+
+@pytest.mark.parametrize("dt", list(DT))
+@pytest.mark.parametrize("M,K", [(1, 1), (1, 7), (3, 8), (5, 255), (2, 256), (4, 1021), (1, 4096), (2, 12001), (3, 40000), (700, 64), (130, 2752)])
+def test_quantize_rows(dt, M, K):
+    g = gen(M * K)
+    for pitch in (0, 8, 5):
+        x, _ = inside((normal(g, (M, K)) * 10.0 ** float(torch.randint(-3, 3, (), generator=g, device="cuda"))).to(DT[dt]), pitch, float("nan"))
+        q, s = pl.quantize_rows(x)
+        wq, ws = quantized(x)
+        equal(q, wq, "codes")
+        equal(s, ws, "scales")
+    out, buf = inside(torch.zeros(M, K, dtype=torch.int8, device="cuda"), 6, 99)
+    pl.quantize_rows(x, q=out)
+    equal(out, wq)
+    buf[:, 3:3 + K] = 99
+    assert (buf == 99).all(), "codes were written between the rows"
+
+
+@pytest.mark.parametrize("dt", list(DT))
+def test_quantize_halfway_values_go_to_even_codes(dt):
+    # max 127: a code is the rounded value itself; x.5 is halfway exactly
+    v = torch.tensor([127.0] + [i + 0.5 for i in range(-64, 64)], device="cuda").to(DT[dt])
+    top = torch.tensor([[1.0], [2.0], [0.25], [-4.0]], device="cuda")
+    x = (v.double() * top).to(DT[dt])
+    q, s = pl.quantize_rows(x)
+    equal(q, (v.double() * top.sign()).round().to(torch.int8).expand(4, -1))
+    equal(s, top.abs().squeeze(-1).float())
+
+
+@pytest.mark.parametrize("dt", list(DT))
+def test_quantize_rows_without_a_finite_largest_value(dt):
+    inf, nan = float("inf"), float("nan")
+    x = torch.ones(6, 300, device="cuda", dtype=DT[dt])
+    x[1] = 0
+    x[2, 299] = inf
+    x[3, 0] = -inf
+    x[4, 150] = nan
+    x[5, 7], x[5, 290] = nan, inf
+    q, s = pl.quantize_rows(x)
+    assert s[0] == torch.tensor(1.0 / 127).item() or abs(s[0].item() * 127 - 1) < 2 ** -23
+    assert (q[0] == 127).all() and s[1] == 0 and (q[1:] == 0).all() and s[2:].isnan().all()
+    y = pl.matmul_i8(q, s, torch.ones(9, 300, dtype=torch.int8, device="cuda"), None, act=B.ACT_RELU, out_dt=ABI[dt])
+    assert (y[1] == 0).all() and y[2:].isnan().all() and y[0].isfinite().all()
+
+
+# ---------------------------------------------------------------------------------------------------------
+# product in 8 bits
+# ---------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("out", list(DT))
+@pytest.mark.parametrize("M,K,N", SHAPES)
+def test_matmul_i8_sums_are_exact(M, K, N, out):
+    g = gen(M + K + N)
+    dt = DT[out]
+    for pitch in (0, 16, 3):
+        a, _ = inside(codes(g, (M, K)), pitch, 77)
+        w, _ = inside(codes(g, (N, K)), pitch, 55)
+        want = (a.double() @ w.double().t()).float().to(dt)  # fp32 first: the sum is converted before it is stored
+        y, buf = inside(torch.zeros(M, N, dtype=dt, device="cuda"), pitch, 7.0)
+        got = pl.matmul_i8(a, None, w, None, out_dt=ABI[out], y=y)
+        assert got is y
+        equal(y, want, "pitch %d" % pitch)
+        if buf is not None:
+            y.fill_(7.0)
+            assert (buf == 7.0).all(), "something was written between the rows"
+
+
+@pytest.mark.parametrize("act_", [0, 1, 2])
+@pytest.mark.parametrize("M,K,N,out", [(1, 500, 40, "bf16"), (19, 64, 33, "f32"), (70, 333, 130, "f16"), (300, 512, 256, "bf16"), (260, 1040, 520, "f32")])
+def test_matmul_i8_output_stage(M, K, N, out, act_):
+    g = gen(M + N + act_)
+    dt = DT[out]
+    a, w = codes(g, (M, K)), codes(g, (N, K))
+    sa, sw = normal(g, (M,)).abs() * 0.01, normal(g, (N,)).abs() * 0.01
+    bias, res = normal(g, (N,)), normal(g, (M, N)).to(dt)
+    lin = (a.double() @ w.double().t()) * sa.double()[:, None] * sw.double()
+    for use_bias in (True, False):
+        for r in (res, None, inside(res, 5, 0.0)[0]):
+            y = pl.matmul_i8(a, sa, w, sw, bias=bias if use_bias else None, act=act_, residual=r, out_dt=ABI[out])
+            v = lin + (bias.double() if use_bias else 0.0)
+            want = act(v, act_) + (0.0 if r is None else r.double())
+            size = lin.abs() + bias.double().abs() + res.double().abs()
+            # conversion, two scales, bias, exponential (|v| + 2), sum, reciprocal with correction (4), residual
+            tol = half_step(dt) * (1 + 2 ** -7) * want.abs() + (12 + v.abs()) * U * size + least(dt)
+            check(y, want, tol)
+
+
+def test_matmul_i8_largest_sums():
+    # the longest sum there is, all of one sign: 131071 * 128 * 128 = 2147467264 stays below 2^31
+    K = (1 << 17) - 1
+    a = torch.full((3, K), -128, dtype=torch.int8, device="cuda")
+    y = pl.matmul_i8(a, None, a, None, out_dt=B.F32)
+    assert (y == float(K * 128 * 128)).all()
+    with pytest.raises(B.RtossError):
+        b = torch.zeros(1, K + 1, dtype=torch.int8, device="cuda")
+        pl.matmul_i8(b, None, b, None)
+
+
+def test_matmul_i8_rows_of_positions():
+    # a channels-last tensor's positions are rows, and so is a channel slice of a wider one
+    g = gen(5)
+    x, w = codes(g, (2, 5, 7, 64)), codes(g, (48, 48))
+    s = normal(g, (2, 5, 7)).abs()
+    y = pl.matmul_i8(x[..., 8:56], s, w, None, out_dt=B.F32)
+    want = (x[..., 8:56].double() @ w.double().t()).float() * s[..., None]
+    assert y.shape == (2, 5, 7, 48)
+    equal(y, want)
+
+
+# ---------------------------------------------------------------------------------------------------------
+# gated block
+# ---------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dt", list(DT))
+@pytest.mark.parametrize("M,K,F", SHAPES)
+def test_gated_ff_of_whole_numbers(M, K, F, dt):
+    """|x| <= 2, |w| <= 1: sums of up to 4096 products are below 2^13 and exact; their product is rounded to fp32 (to 24 bits: exact below
+    2^24, else rounded once more before the store, as the reference does)."""
+    g = gen(M * 3 + K * 5 + F)
+    t = DT[dt]
+    for pitch in (0, 8, 3):
+        x, _ = inside(whole(g, (M, K), 2, t), pitch, float("nan"))
+        wg, _ = inside(whole(g, (F, K), 1, t), pitch, float("nan"))
+        wu, _ = inside(whole(g, (F, K), 1, t), pitch, float("nan"))
+        G, V = x.double() @ wg.double().t(), x.double() @ wu.double().t()
+        for a in (0, 1):
+            want = (act(G, a) * V).float().to(t)
+            hb, buf = inside(torch.zeros(M, F, dtype=t, device="cuda"), pitch, 7.0)
+            equal(pl.gated_ff(x, wg, wu, act=a, h=hb), want, "h, pitch %d" % pitch)
+            if buf is not None:
+                hb.fill_(7.0)
+                assert (buf == 7.0).all(), "something was written between the rows"
+        h, gate, up = pl.gated_ff(x, wg, wu, act=1, keep=True)
+        equal(h, (act(G, 1) * V).float().to(t))
+        equal(gate, G.to(t))
+        equal(up, V.to(t))
+
+
+@pytest.mark.parametrize("dt", list(DT))
+@pytest.mark.parametrize("M,K,F", [(1, 700, 50), (4, 2048, 72), (40, 96, 130), (260, 512, 264), (77, 333, 129), (600, 256, 520)])
+def test_gated_ff_silu(M, K, F, dt):
+    g = gen(M + K + F)
+    t = DT[dt]
+    x, wg, wu = normal(g, (M, K)).to(t), normal(g, (F, K), K ** -0.5).to(t), normal(g, (F, K), K ** -0.5).to(t)
+    wg[0] *= 300  # gates far out on both sides
+    h, gate, up = pl.gated_ff(x, wg, wu, keep=True)
+    G, V = x.double() @ wg.double().t(), x.double() @ wu.double().t()
+    # a sum of K products: every addition rounds what has come together so far (twice that, for sums that are cut off instead)
+    eg = 2 * (K + 4) * U * (x.double().abs() @ wg.double().abs().t())
+    eu = 2 * (K + 4) * U * (x.double().abs() @ wu.double().abs().t())
+    check(gate, G, eg + half_step(t) * (G.abs() + eg) + least(t), "gate")
+    check(up, V, eu + half_step(t) * (V.abs() + eu) + least(t), "up")
+    want = act(G, 2) * V
+    # |act'| <= 1.1; the exponential |g| + 2, the quotient 4, the product 1
+    tol = 1.1 * eg * V.abs() + act(G, 2).abs() * eu + 1.1 * eg * eu + (8 + G.abs()) * U * want.abs()
+    check(h, want, tol + half_step(t) * (want.abs() + tol) + least(t), "h")
+
+
+@pytest.mark.parametrize("out", list(DT))
+@pytest.mark.parametrize("M,K,F", SHAPES)
+def test_gated_ff_i8(M, K, F, out):
+    g = gen(M + 7 * K + F)
+    t = DT[out]
+    pitch = (0, 16, 5)[(M + K + F) % 3]
+    a, _ = inside(codes(g, (M, K)), pitch, 1)
+    wg, _ = inside(codes(g, (F, K)), pitch, 1)
+    wu, _ = inside(codes(g, (F, K)), pitch, 1)
+    scale = 3.0 / (5000 * K ** 0.5)
+    sa = normal(g, (M,)).abs() * scale ** 0.5
+    sg, su = normal(g, (2, F)).abs() * scale ** 0.5
+    G = (a.double() @ wg.double().t()) * sa.double()[:, None] * sg.double()
+    V = (a.double() @ wu.double().t()) * sa.double()[:, None] * su.double()
+    for act_ in (0, 2):
+        h = pl.gated_ff_i8(a, sa, wg, sg, wu, su, act=act_, out_dt=ABI[out])
+        want = act(G, act_) * V
+        # conversion and two scales on both sides, exponential, quotient, product
+        tol = (14 + 2 * G.abs()) * U * G.abs() * V.abs()
+        check(h, want, tol + half_step(t) * (want.abs() + tol) + least(t), "act %d" % act_)
+    equal(pl.gated_ff_i8(a, None, wg, None, wu, None, act=1, out_dt=B.F32),
+          torch.relu((a.double() @ wg.double().t()).float()) * (a.double() @ wu.double().t()).float())
+
+
+# ---------------------------------------------------------------------------------------------------------
+# gradients
+# ---------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dt", list(DT))
+@pytest.mark.parametrize("M,K,F", SHAPES)
+def test_gradients_of_whole_numbers(M, K, F, dt):
+    """Values of at most 2: dg and du are at most 4, sums of up to 2 * 640 or 1030 products of at most 8 exact."""
+    g = gen(M + 11 * K + F)
+    t = DT[dt]
+    for pitch in (0, 8, 3):
+        x, _ = inside(whole(g, (M, K), 2, t), pitch, float("nan"))
+        wg, _ = inside(whole(g, (F, K), 2, t), pitch, float("nan"))
+        wu, _ = inside(whole(g, (F, K), 2, t), pitch, float("nan"))
+        dh, _ = inside(whole(g, (M, F), 2, t), pitch, float("nan"))
+        gate, up = whole(g, (M, F), 2, t), whole(g, (M, F), 2, t)
+        for a in (0, 1):
+            dg = dh.double() * up.double() * ((gate > 0).double() if a else 1.0)
+            du = dh.double() * act(gate.double(), a)
+            dx, dwg, dwu = pl.gated_ff_backward(dh, x, wg, wu, gate, up, act=a)
+            equal(dx, (dg @ wg.double() + du @ wu.double()).to(t), "dx, pitch %d" % pitch)
+            equal(dwg, (dg.t() @ x.double()).to(t), "dw_gate, pitch %d" % pitch)
+            equal(dwu, (du.t() @ x.double()).to(t), "dw_up, pitch %d" % pitch)
+
+
+def _silu_slope(v):
+    s = torch.sigmoid(v)
+    return s * (1 + v * (1 - s))
+
+
+@pytest.mark.parametrize("dt", list(DT))
+@pytest.mark.parametrize("M,K,F", [(1, 40, 30), (37, 64, 96), (130, 264, 200), (515, 96, 136), (300, 333, 129)])
+def test_gradients_silu(M, K, F, dt):
+    g = gen(M + K * F)
+    t = DT[dt]
+    x, wg, wu = normal(g, (M, K)).to(t), normal(g, (F, K), K ** -0.5).to(t), normal(g, (F, K), K ** -0.5).to(t)
+    gate, up, dh = normal(g, (M, F), 2.0).to(t), normal(g, (M, F)).to(t), normal(g, (M, F)).to(t)
+    gate[0, :3] = torch.tensor([-120.0, 120.0, 0.0], device="cuda")
+    dx, dwg, dwu = pl.gated_ff_backward(dh, x, wg, wu, gate, up)
+    G, V, H = gate.double(), up.double(), dh.double()
+    dg, du = H * V * _silu_slope(G), H * act(G, 2)
+    # s, in units of 2^-24: exponential |g| + 2, sum, reciprocal (1 ulp = 2); act' = s (1 + g (1 - s)) within |g| + 9 of (1 + |g|) s; the
+    # products; then the rounding to the operands' type
+    s = torch.sigmoid(G)
+    eg = H.abs() * V.abs() * ((2 * G.abs() + 12) * U * (1 + G.abs()) * s.clamp_min(1e-30))
+    eu = (G.abs() + 8) * U * du.abs()
+    eg, eu = eg + half_step(t) * (dg.abs() + eg) + least(t), eu + half_step(t) * (du.abs() + eu) + least(t)
+
+    def close(got, want, first, second, size, n, what):
+        tol = first + second + 2 * (n + 4) * U * size
+        check(got, want, tol + half_step(t) * (want.abs() + tol) + least(t), what)
+
+    W, X, Wu = wg.double(), x.double(), wu.double()
+    close(dx, dg @ W + du @ Wu, eg @ W.abs(), eu @ Wu.abs(), (dg.abs() + eg) @ W.abs() + (du.abs() + eu) @ Wu.abs(), 2 * F, "dx")
+    close(dwg, dg.t() @ X, eg.t() @ X.abs(), 0.0, (dg.abs() + eg).t() @ X.abs(), M, "dw_gate")
+    close(dwu, du.t() @ X, eu.t() @ X.abs(), 0.0, (du.abs() + eu).t() @ X.abs(), M, "dw_up")
+
+
+@pytest.mark.parametrize("a", [0, 1, 2])
+def test_gradients_against_differences(a):
+    """Along a direction, the kernels' gradient is the slope of sum(dh * h) as differences of the block in 64 bits give it: central, off by
+    the third derivative times step^2 / 6."""
+    g = gen(70 + a)
+    M, K, F = 20, 36, 44
+    x, wg, wu, dh = normal(g, (M, K)), normal(g, (F, K), K ** -0.5), normal(g, (F, K), K ** -0.5), normal(g, (M, F))
+    _, gate, up = pl.gated_ff(x, wg, wu, act=a, keep=True)
+    grads = pl.gated_ff_backward(dh, x, wg, wu, gate, up, act=a)
+
+    def loss(x, wg, wu):
+        return (dh.double() * act(x @ wg.t(), a) * (x @ wu.t())).sum()
+
+    at = [t.double() for t in (x, wg, wu)]
+    step = 1e-6
+    for i, grad in enumerate(grads):
+        d = normal(g, at[i].shape).double()
+        if a == 1:  # gates closer to 0 than the step moves them have no slope: 1e-6 against gates of order 1
+            move = [torch.zeros_like(t) for t in at]
+            move[i] = d
+            assert ((x.double() @ move[1].t() + move[0] @ wg.double().t()).abs() * step < gate.double().abs()).all()
+        hi, lo = list(at), list(at)
+        hi[i], lo[i] = at[i] + step * d, at[i] - step * d
+        slope = (loss(*hi) - loss(*lo)).item() / (2 * step)
+        size = (grad.double().abs() * d.abs()).sum().item()
+        # 64-bit sums of M * F terms lose 2^-53 * M * F of some 10^3 over 2 * step; the kernels K + M + F roundings of fp32
+        assert abs((grad.double() * d).sum().item() - slope) < 1e-5 * size
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_gradients_on_request_and_of_no_rows(dt):
+    g = gen(3)
+    t = DT[dt]
+    x, wg, wu = whole(g, (50, 64), 2, t), whole(g, (72, 64), 2, t), whole(g, (72, 64), 2, t)
+    gate, up, dh = (whole(g, (50, 72), 2, t) for _ in range(3))
+    every = pl.gated_ff_backward(dh, x, wg, wu, gate, up)
+    dx, a, b = pl.gated_ff_backward(dh, x, wg, wu, gate, up, weights=False)
+    assert a is None and b is None
+    equal(dx, every[0])
+    none, a, b = pl.gated_ff_backward(dh, x, wg, wu, gate, up, rows=False)
+    assert none is None
+    equal(a, every[1])
+    equal(b, every[2])
+    dx, a, b = pl.gated_ff_backward(dh[:0], x[:0], wg, wu, gate[:0], up[:0])
+    assert dx.shape == (0, 64) and (a == 0).all() and (b == 0).all() and a.shape == wg.shape
+    assert pl.gated_ff(x[:0], wg, wu).shape == (0, 72)
+    q, s = pl.quantize_rows(x[:0])
+    assert q.shape == (0, 64) and s.shape == (0,)
+    wq, ws = pl.quantize_rows(wg)
+    assert pl.matmul_i8(q, s, wq, ws).shape == (0, 72) and pl.gated_ff_i8(q, s, wq, ws, wq, ws).shape == (0, 72)
+
+
+# ---------------------------------------------------------------------------------------------------------
+# as they are used
+# ---------------------------------------------------------------------------------------------------------
+def _served(x, weights, out=B.BF16):
+    wg, sg, wu, su, wd, sd = weights
+    q, s = pl.quantize_rows(x)
+    h = pl.gated_ff_i8(q, s, wg, sg, wu, su, out_dt=out)
+    q, s = pl.quantize_rows(h)
+    return pl.matmul_i8(q, s, wd, sd, residual=x, out_dt=out)
+
+
+def _weights(g, K, F):
+    out = []
+    for shape in ((F, K), (F, K), (K, F)):
+        out += pl.quantize_rows(normal(g, shape, shape[1] ** -0.5))
+    return out
+
+
+@pytest.mark.parametrize("M,K,F", [(1, 256, 704), (5, 200, 520), (90, 128, 352), (300, 256, 704)])
+def test_served_block(M, K, F):
+    """The block in 8 bits against the same steps in 64: the codes of the hidden values differ where their last bit does, by one of 127."""
+    g = gen(M)
+    weights = _weights(g, K, F)
+    x = normal(g, (M, K)).to(torch.bfloat16)
+    y = _served(x, weights)
+    wg, sg, wu, su, wd, sd = [t.double() for t in weights]
+    q, s = quantized(x)
+    q, s = q.double(), s.double()[:, None]
+    h = act((q @ wg.t()) * s * sg, 2) * ((q @ wu.t()) * s * su)
+    size = (8 + (q @ wg.t()).abs() * s * sg) * U * h.abs()
+    step = half_step(torch.bfloat16) * 2 * (h.abs() + size)  # one step of a hidden value
+    top = h.abs().amax(1, keepdim=True)
+    # a code is off by half from the quotient, and moves with its value and with the largest one
+    eh = (0.5 / 127) * top * (1 + 2 ** -6) + step + size
+    want = h @ (wd * sd[:, None]).t() + x.double()
+    check(y, want, eh @ (wd.abs() * sd[:, None]).t() + half_step(torch.bfloat16) * (want.abs() + 1) + 1e-5 * (h.abs() @ (wd.abs() * sd[:, None]).t()))
+
+
+def test_training_step():
+    """Forward and backward as a step of training runs them: bf16 tensors, gradients against autograd of the plain block in 64 bits.  The kept
+    projections, dg and du are rounded to bf16 (2^-8 of the value each) and so are the gradients; the 2-norm of the difference stays
+    below the sum of the four."""
+    g = gen(11)
+    M, K, F = 384, 256, 704
+    x, wg, wu = normal(g, (M, K)).bfloat16(), normal(g, (F, K), K ** -0.5).bfloat16(), normal(g, (F, K), K ** -0.5).bfloat16()
+    h, gate, up = pl.gated_ff(x, wg, wu, keep=True)
+    dh = normal(g, (M, F)).bfloat16()
+    grads = pl.gated_ff_backward(dh, x, wg, wu, gate, up)
+    leaves = [t.double().requires_grad_(True) for t in (x, wg, wu)]
+    (act(leaves[0] @ leaves[1].t(), 2) * (leaves[0] @ leaves[2].t())).backward(dh.double())
+    for got, leaf in zip(grads, leaves):
+        assert (got.double() - leaf.grad).norm() <= 4 * 2.0 ** -8 * leaf.grad.norm()
+
+
+def test_replays_of_a_captured_run_match_eager():
+    g = gen(21)
+    M, K, F = 70, 256, 704
+    weights = _weights(g, K, F)
+    wg, wu = normal(g, (F, K), K ** -0.5).bfloat16(), normal(g, (F, K), K ** -0.5).bfloat16()
+    xs = [normal(g, (M, K)).bfloat16() for _ in range(3)]
+    x, dh = xs[0].clone(), normal(g, (M, F)).bfloat16()
+
+    def run():
+        h, gate, up = pl.gated_ff(x, wg, wu, keep=True)
+        return [_served(x, weights), h, *pl.gated_ff_backward(dh, x, wg, wu, gate, up)]
+
+    eager = []
+    for v in xs:
+        x.copy_(v)
+        eager.append(run())
+    torch.cuda.synchronize()
+    graphs, outs = [], []
+    for _ in range(2):  # two graphs: neither may depend on memory of the other
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            outs.append(run())
+        graphs.append(graph)
+    for rep in range(6):
+        i = rep % 3
+        x.copy_(xs[i])
+        run()  # eager work between the replays
+        for graph, out in zip(graphs, outs):
+            for t in out:
+                t.zero_()
+            torch.cuda.synchronize()
+            graph.replay()
+            torch.cuda.synchronize()
+            for got, want in zip(out, eager[i]):
+                equal(got, want, "replay %d" % rep)
+
+
+def test_other_streams_and_two_calls_at_once():
+    g = gen(31)
+    x = [normal(g, (130, 512)).bfloat16() for _ in range(2)]
+    weights = _weights(g, 512, 1000)
+    want = [_served(t, weights) for t in x]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got = [[], []]
+    for _ in range(5):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i].append(_served(x[i], weights))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for t in got[i]:
+            equal(t, want[i])
+
+
+def test_same_call_gives_the_same_bits():
+    g = gen(41)
+    x, wg, wu = normal(g, (700, 300)), normal(g, (520, 300)), normal(g, (520, 300))
+    first = pl.gated_ff(x, wg, wu, keep=True)
+    grads = pl.gated_ff_backward(first[0], x, wg, wu, first[1], first[2])
+    for _ in range(3):
+        again = pl.gated_ff(x, wg, wu, keep=True)
+        for a, b in zip(first, again):
+            equal(a, b)
+        for a, b in zip(grads, pl.gated_ff_backward(first[0], x, wg, wu, first[1], first[2])):
+            equal(a, b)
+
+
+def test_rows_past_the_last_and_workspaces_of_the_caller():
+    """Results inside larger buffers: what lies behind the last row stays.  The workspace is the caller's, of the size asked for."""
+    g = gen(51)
+    t = torch.bfloat16
+    M, K, F = 33, 96, 80
+    x, wg, wu = whole(g, (M, K), 2, t), whole(g, (F, K), 1, t), whole(g, (F, K), 1, t)
+    buf = torch.full((M + 300, F), 7.0, dtype=t, device="cuda")
+    pl.gated_ff(x, wg, wu, h=buf[:M])
+    assert (buf[M:] == 7.0).all()
+    dh, gate, up = (whole(g, (M, F), 2, t) for _ in range(3))
+    n = B.rtoss_gated_ff_backward_size(B.GatedDesc(M, K, F, B.BF16, B.ACT_SILU, 0, 0, 0))
+    space = torch.full((n + 4096,), 201, dtype=torch.uint8, device="cuda")
+    a = pl.gated_ff_backward(dh, x, wg, wu, gate, up, workspace=space[:n])
+    assert (space[n:] == 201).all()
+    for p, q in zip(a, pl.gated_ff_backward(dh, x, wg, wu, gate, up)):
+        equal(p, q)
+    with pytest.raises(B.RtossError):
+        pl.gated_ff_backward(dh, x, wg, wu, gate, up, workspace=space[:n - 1])
+
+
+def test_offsets_past_32_bits():
+    """Rows far apart: the last ones start more than 2^32 bytes behind the first."""
+    g = gen(61)
+    M, K, N = 70, 64, 48
+    ld = 1 << 26
+    big = torch.empty(M, ld, dtype=torch.int8, device="cuda")
+    big[:, :K] = codes(g, (M, K))
+    w = codes(g, (N, K))
+    equal(pl.matmul_i8(big[:, :K], None, w, None, out_dt=B.F32), (big[:, :K].double() @ w.double().t()).float())
+    wide = big.view(torch.bfloat16)[:, :ld // 2]
+    x = wide[:, :K]
+    x.copy_(whole(g, (M, K), 2))
+    wg, wu = whole(g, (N, K), 1, torch.bfloat16), whole(g, (N, K), 1, torch.bfloat16)
+    h = wide[:, 4096:4096 + N]
+    G, V = x.double() @ wg.double().t(), x.double() @ wu.double().t()
+    equal(pl.gated_ff(x, wg, wu, act=0, h=h), (G * V).to(torch.bfloat16))
+    q, s = pl.quantize_rows(x)
+    equal(q, quantized(x)[0])
+    dh, gate, up = h, whole(g, (M, N), 1, torch.bfloat16), whole(g, (M, N), 1, torch.bfloat16)
+    dh.copy_(whole(g, (M, N), 2))
+    dx, dwg, dwu = pl.gated_ff_backward(dh, x, wg, wu, gate, up, act=0)
+    dg, du = dh.double() * up.double(), dh.double() * gate.double()
+    equal(dx, (dg @ wg.double() + du @ wu.double()).to(torch.bfloat16))
+    equal(dwg, (dg.t() @ x.double()).to(torch.bfloat16))
+    equal(dwu, (du.t() @ x.double()).to(torch.bfloat16))
+
+
+def test_refusals_of_tensors():
+    x, w = torch.zeros(4, 16, device="cuda"), torch.zeros(8, 16, device="cuda")
+    q, s = pl.quantize_rows(x)
+    wq, ws = pl.quantize_rows(w)
+    bad = [lambda: pl.quantize_rows(x.t()), lambda: pl.quantize_rows(x[:1].expand(4, 16)), lambda: pl.quantize_rows(x, q=q[:3]),
+           lambda: pl.matmul_i8(q, s, wq[:, :8], ws), lambda: pl.matmul_i8(q, s[:3], wq, ws), lambda: pl.matmul_i8(q, s.double(), wq, ws),
+           lambda: pl.matmul_i8(q, s, wq, ws, bias=ws[:4]), lambda: pl.matmul_i8(q, s, wq, ws, residual=x),
+           lambda: pl.matmul_i8(x, s, wq, ws), lambda: pl.gated_ff(x, w, w[:4]), lambda: pl.gated_ff(x, w, w.half()),
+           lambda: pl.gated_ff(x, w[:, :8], w[:, :8]), lambda: pl.gated_ff(x, w, w, h=torch.zeros(4, 9, device="cuda")),
+           lambda: pl.gated_ff(x, w, w.cpu()), lambda: pl.gated_ff(x, w, torch.zeros(8, 32, device="cuda")[:, :16]),
+           lambda: pl.gated_ff_backward(x, x, w, w, x, x)]
+    for i, call in enumerate(bad):
+        with pytest.raises(AssertionError):
+            call()
+            pytest.fail("call %d was not refused" % i)
+    with pytest.raises(B.RtossError):
+        pl.gated_ff(x, w, w, act=5)
+    with pytest.raises(TypeError):
+        pl.quantize_rows(x.double())
