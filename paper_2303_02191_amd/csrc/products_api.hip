@@ -73,6 +73,12 @@ rtoss_status gated_desc(const rtoss_gated_desc* desc, rtoss_gated_desc* d)
     return RTOSS_OK;
 }
 
+rtoss_status launch_product(ProductForm form, bool bits8, rtoss_dtype out, const Product& p, hipStream_t s)
+{
+    if (p.M > 128 && product_tiles_ok(form, bits8, out, p)) return launch_product_tiles(form, bits8, out, p, s);
+    return launch_product_any(form, bits8, out, p, s);
+}
+
 size_t slopes_bytes(const rtoss_gated_desc& d) { return align_up((size_t)d.M * d.F * elem_bytes(d.dt), 256); }
 
 }  // namespace
@@ -144,7 +150,7 @@ rtoss_status rtoss_matmul_i8(const rtoss_matmul_desc* desc, const int8_t* a_dev,
     p.y = y_dev;
     p.ldr = residual_ld;
     p.ldy = y_ld;
-    return launch_product_any(kScaled, true, d.out_dt, p, (hipStream_t)hip_stream);
+    return launch_product(kScaled, true, d.out_dt, p, (hipStream_t)hip_stream);
 }
 
 rtoss_status rtoss_gated_ff(const rtoss_gated_desc* desc, const void* x_dev, const void* w_gate_dev, const void* w_up_dev, void* h_dev,
@@ -182,7 +188,7 @@ rtoss_status rtoss_gated_ff(const rtoss_gated_desc* desc, const void* x_dev, con
     p.y0 = gate_dev;
     p.y1 = up_dev;
     p.ldy = d.h_ld;
-    return launch_product_any(kGated, false, d.dt, p, (hipStream_t)hip_stream);
+    return launch_product(kGated, false, d.dt, p, (hipStream_t)hip_stream);
 }
 
 rtoss_status rtoss_gated_ff_i8(const rtoss_gated_desc* desc, const int8_t* a_dev, const float* a_scale_dev, const int8_t* w_gate_dev,
@@ -217,7 +223,7 @@ rtoss_status rtoss_gated_ff_i8(const rtoss_gated_desc* desc, const int8_t* a_dev
     p.s1 = up_scale_dev;
     p.y = h_dev;
     p.ldy = d.h_ld;
-    return launch_product_any(kGated, true, d.dt, p, (hipStream_t)hip_stream);
+    return launch_product(kGated, true, d.dt, p, (hipStream_t)hip_stream);
 }
 
 rtoss_status rtoss_gated_ff_backward_size(const rtoss_gated_desc* desc, size_t* workspace_bytes)
@@ -282,7 +288,7 @@ rtoss_status rtoss_gated_ff_backward(const rtoss_gated_desc* desc, const void* d
         p.R = d.F;
         p.y = dx_dev;
         p.ldy = d.K;
-        RTOSS_TRY(launch_product_any(kBackRows, false, d.dt, p, s));
+        RTOSS_TRY(launch_product(kBackRows, false, d.dt, p, s));
     }
     if (weights) {
         p.b0 = x_dev;
@@ -293,7 +299,7 @@ rtoss_status rtoss_gated_ff_backward(const rtoss_gated_desc* desc, const void* d
         p.y = dw_gate_dev;
         p.y1 = dw_up_dev;
         p.ldy = d.K;
-        RTOSS_TRY(launch_product_any(kBackWeights, false, d.dt, p, s));
+        RTOSS_TRY(launch_product(kBackWeights, false, d.dt, p, s));
     }
     return RTOSS_OK;
 }
