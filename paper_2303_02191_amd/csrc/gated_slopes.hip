@@ -28,48 +28,58 @@ template <typename T, int ACT> __device__ __forceinline__ void slopes(float g, f
     }
 }
 
-// VEC: 16 bytes a lane and step; `n` elements in one run (dh as wide as a row), all starts aligned to 16 bytes.
+// A lane takes 16 bytes of dg and du at a time, row by row; ldd is a whole number of such pieces, with zeros past the row's end.  VEC: so
+// are the rows of the inputs.
 template <typename T, int ACT, bool VEC>
 __global__ __launch_bounds__(256) void gated_slopes_kernel(const T* __restrict__ dh, const T* __restrict__ gate, const T* __restrict__ up,
-                                                           T* __restrict__ dg, T* __restrict__ du, int64_t n, int F, int64_t ldh)
+                                                           T* __restrict__ dg, T* __restrict__ du, int64_t pieces, int per_row, int F, int64_t ldh)
 {
-    constexpr int E = VEC ? 16 / (int)sizeof(T) : 1;
-    const int64_t step = (int64_t)gridDim.x * 256 * E;
-    for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * E; i < n; i += step) {
-        if (VEC && i + E <= n) {
-            T g[E], u[E], h[E], og[E], ou[E];
-            *(u32x4*)g = *(const u32x4*)(gate + i);
-            *(u32x4*)u = *(const u32x4*)(up + i);
-            *(u32x4*)h = *(const u32x4*)(dh + i);
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                float a, b;
-                slopes<T, ACT>(to_f32(g[e]), to_f32(u[e]), to_f32(h[e]), a, b);
-                store_from_f32(og + e, a);
-                store_from_f32(ou + e, b);
-            }
-            *(u32x4*)(dg + i) = *(u32x4*)og;
-            *(u32x4*)(du + i) = *(u32x4*)ou;
+    constexpr int E = 16 / (int)sizeof(T);
+    const int64_t step = (int64_t)gridDim.x * 256;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < pieces; i += step) {
+        T g[E], u[E], h[E], og[E], ou[E];
+        if (VEC && ldh == F) {  // one run: no rows to find
+            *(u32x4*)g = *(const u32x4*)(gate + i * E);
+            *(u32x4*)u = *(const u32x4*)(up + i * E);
+            *(u32x4*)h = *(const u32x4*)(dh + i * E);
         } else {
-            for (int64_t j = i; j < n && j < i + E; ++j) {
-                float a, b;
-                const int64_t at = VEC ? j : j / F * ldh + j % F;
-                slopes<T, ACT>(to_f32(gate[j]), to_f32(up[j]), to_f32(dh[at]), a, b);
-                store_from_f32(dg + j, a);
-                store_from_f32(du + j, b);
+            const int64_t m = i / per_row;
+            const int f = (int)(i - m * per_row) * E;
+            const T *pg = gate + m * F + f, *pu = up + m * F + f, *ph = dh + m * ldh + f;
+            if (f + E <= F) {  // (at whatever address)
+                __builtin_memcpy(g, pg, 16);
+                __builtin_memcpy(u, pu, 16);
+                __builtin_memcpy(h, ph, 16);
+            } else {
+#pragma unroll
+                for (int e = 0; e < E; ++e) g[e] = u[e] = h[e] = T{};
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    if (f + e < F) g[e] = pg[e], u[e] = pu[e], h[e] = ph[e];
             }
         }
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            float a, b;
+            slopes<T, ACT>(to_f32(g[e]), to_f32(u[e]), to_f32(h[e]), a, b);
+            store_from_f32(og + e, a);
+            store_from_f32(ou + e, b);
+        }
+        *(u32x4*)(dg + i * E) = *(u32x4*)og;
+        *(u32x4*)(du + i * E) = *(u32x4*)ou;
     }
 }
 
 template <typename T>
-rtoss_status launch(rtoss_act act, int64_t n, int F, const void* dh, int64_t ldh, const void* gate, const void* up, void* dg, void* du, hipStream_t s)
+rtoss_status launch(rtoss_act act, int64_t M, int F, const void* dh, int64_t ldh, const void* gate, const void* up, void* dg, void* du, hipStream_t s)
 {
-    const bool vec = ldh == F && ((uintptr_t)dh | (uintptr_t)gate | (uintptr_t)up | (uintptr_t)dg | (uintptr_t)du) % 16 == 0;
-    const int64_t per = 256 * (vec ? 16 / (int)sizeof(T) : 1);
-    const unsigned grid = (unsigned)std::min<int64_t>((n + per - 1) / per, 16384);
+    constexpr int E = 16 / (int)sizeof(T);
+    const bool vec = F % E == 0 && ((uintptr_t)dh | (uintptr_t)gate | (uintptr_t)up) % 16 == 0;
+    const int per_row = (F + E - 1) / E;
+    const int64_t pieces = M * per_row;
+    const unsigned grid = (unsigned)std::min<int64_t>((pieces + 255) / 256, 16384);
     auto go = [&](auto kernel) {
-        kernel<<<grid, 256, 0, s>>>((const T*)dh, (const T*)gate, (const T*)up, (T*)dg, (T*)du, n, F, ldh);
+        kernel<<<grid, 256, 0, s>>>((const T*)dh, (const T*)gate, (const T*)up, (T*)dg, (T*)du, pieces, per_row, F, ldh);
         return check_hip(hipGetLastError(), "gated_slopes launch");
     };
     switch (act) {
@@ -84,11 +94,10 @@ rtoss_status launch(rtoss_act act, int64_t n, int F, const void* dh, int64_t ldh
 rtoss_status launch_gated_slopes(rtoss_dtype dt, rtoss_act act, int64_t M, int F, const void* dh, int64_t ldh, const void* gate, const void* up,
                                  void* dg, void* du, hipStream_t s)
 {
-    const int64_t n = M * F;
     switch (dt) {
-    case RTOSS_F32: return launch<float>(act, n, F, dh, ldh, gate, up, dg, du, s);
-    case RTOSS_F16: return launch<f16_t>(act, n, F, dh, ldh, gate, up, dg, du, s);
-    default: return launch<bf16_t>(act, n, F, dh, ldh, gate, up, dg, du, s);
+    case RTOSS_F32: return launch<float>(act, M, F, dh, ldh, gate, up, dg, du, s);
+    case RTOSS_F16: return launch<f16_t>(act, M, F, dh, ldh, gate, up, dg, du, s);
+    default: return launch<bf16_t>(act, M, F, dh, ldh, gate, up, dg, du, s);
     }
 }
 

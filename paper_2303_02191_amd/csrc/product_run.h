@@ -7,8 +7,10 @@ namespace rtoss {
 // N neighbouring values of a row, `left` of which exist; vec: the row's runs are aligned to 16 bytes.
 template <typename TO, int N> __device__ __forceinline__ void store_run(TO* p, const float (&v)[N], int left, bool vec)
 {
+    static_assert(N % 8 == 0 || N == 4, "whole pieces of 16 bytes, or half of one");
     if (vec && left >= N) {
         constexpr int E = 16 / (int)sizeof(TO);
+        if constexpr (N < E) *(uint2*)p = uint2{pack2_from_f32<TO>(v[0], v[1]), pack2_from_f32<TO>(v[2], v[3])};
 #pragma unroll
         for (int i = 0; i < N / E; ++i) {
             if constexpr (sizeof(TO) == 4) *(f32x4*)(p + i * E) = f32x4{v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]};
@@ -22,6 +24,7 @@ template <typename TO, int N> __device__ __forceinline__ void store_run(TO* p, c
 }
 template <typename TO, int N> __device__ __forceinline__ void add_run(const TO* p, float (&v)[N], int left, bool vec)
 {
+    static_assert(N % 8 == 0, "whole pieces of 16 bytes");
     if (vec && left >= N) {
         constexpr int E = 16 / (int)sizeof(TO);
 #pragma unroll

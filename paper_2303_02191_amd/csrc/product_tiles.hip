@@ -1,4 +1,29 @@
-// Products of whole 16-byte pieces in tiles of 256 x 256 results: the 8-bit product and the gated block where there are rows enough.
+// Products of whole 16-byte pieces in tiles of 256 x 256 results: the 8-bit product, the gated block and its gradients where there are
+// rows enough.  Bound: the matrix instructions.
+//
+// A workgroup is eight waves, two per SIMD; wave (wm, wn) of 2 x 4 owns 128 x 64 results (128 accumulator registers).  The sum runs over
+// stages of 128 bytes of a row, two buffers of 64 KB in LDS, each in four regions: the halves of the left and of the right operand.  A
+// stage is four quadrants (half of the wave's rows x half of its channels, 16 matrix instructions for two steps of the sum), and a
+// quadrant two parts with a barrier behind each: reading operands and starting copies, and multiplying.  The waves of wm = 1 run one
+// part behind those of wm = 0, so that on every SIMD one wave multiplies while the other reads.
+//   - Quadrants run (0, x) (0, y) (1, y) (1, x); x is the half whose operands are there from the stage before, where they were read
+//     beside the last quadrant into the registers of y.  So a quadrant reads 8, 4, 8, 4 vectors of 1 KB a wave, 256 cycles of LDS at most
+//     for four waves, beside 256 cycles of matrix instructions.
+//   - Number the quadrants p and the regions in the order of their use, j (x of B, half 0 of A, y of B, half 1 of A): p reads
+//     region p + 1 and starts the copies of p + 7, whose place the region p - 1 had, read in quadrant p - 2: its reads were waited for by
+//     both groups of waves a barrier ago.  A region has six quadrants, some 3000 cycles, to arrive; the wait of quadrant p covers
+//     region p + 2, in front of a barrier of both groups that precedes its reads.
+// Behind the last stage the last one is copied again into free regions, so that every wait can count copies.
+//
+// Operands that memory holds by rows of the sum's direction (weights and rows of the forward pass) lie in LDS as rows of 128 bytes, those
+// that it holds across (weights in the gradient of the rows; both in that of the weights) as 128 columns of each of the stage's
+// rows, and are transposed by the read (ds_read_b64_tr_b16: lane 4k + j of 16 gives the address of four columns, lane i gets
+// column i of the four rows that lanes 4k .. 4k+3 name, k = 0 .. 3; fp32: one element per read).  Pieces of 16 bytes are
+// exchanged within a row so that the reads spread over the banks.
+//
+// Measured: 8-bit 8192 x 8192 x 8192 with residual 447 us (2.46 POP/s; a library product without the output stage 2.06), gated block bf16
+// 8192 rows x 4096 -> 10944 with both projections kept 1143 us (1.28 PFLOP/s, 1.5 is what a library product of 8192^3 reaches), its gradients
+// with dg and du 2521 us (1.17 PFLOP/s; library products of operands that lie across 1.17 and 1.03).
 #include <algorithm>
 
 #include "product_run.h"
@@ -27,13 +52,64 @@ struct Source {
     }
 };
 
+// The elements r .. r+E-1 of the sum that a lane holds of a fragment, of which `valid` exist: zeros for the others.
+template <typename T> __device__ __forceinline__ void keep_first(u32x4& f, int valid)
+{
+    constexpr int E = 4 / (int)sizeof(T);  // of a word
+#pragma unroll
+    for (int d = 0; d < 4; ++d) {
+        const int have = valid - d * E;
+        const uint32_t mask = have >= E ? ~0u : have <= 0 ? 0u : (1u << (have * 8 * (int)sizeof(T) & 31)) - 1;
+        f[d] &= mask;
+    }
+}
+
+// Reads of an operand that lies across: [rows of the sum][128 columns].
+template <typename T> struct Across {
+    static constexpr int kRowBytes = 128 * (int)sizeof(T);  // (a region: 64 rows of a 16-bit type, 32 of fp32)
+    static constexpr int kReads = sizeof(T) == 4 ? 4 : 2;   // per fragment
+    // place of the 16-byte piece `piece` of row r
+    static __device__ __forceinline__ int spread(int r) { return sizeof(T) == 4 ? (r >> 2 & 3) << 2 : ((r & 3) | (r >> 1 & 4)) << 1; }
+    // a lane's address of the fragment of columns 16 t .. 16 t + 15 in step 0
+    static __device__ __forceinline__ int address(int t, int c, int q)
+    {
+        if constexpr (sizeof(T) == 4) return 4 * q * kRowBytes + ((4 * t ^ spread(4 * q)) * 16) + 4 * c;
+        const int r = 8 * q + (c >> 2);
+        return r * kRowBytes + ((2 * t ^ spread(r)) * 16) + (c & 3) * 8;
+    }
+    static __device__ __forceinline__ u32x4 read(const char* at)  // + step * (half a region)
+    {
+        u32x4 f;
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) f[e] = *(const uint32_t*)(at + e * kRowBytes);
+        } else {
+            typedef short s4 __attribute__((ext_vector_type(4)));
+            typedef __attribute__((address_space(3))) s4* Lds;
+            const uint2 lo = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)at));
+            const uint2 hi = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(at + 4 * kRowBytes)));
+            f = u32x4{lo.x, lo.y, hi.x, hi.y};
+        }
+        return f;
+    }
+};
+
+// 16 bytes a lane from a bounded buffer to LDS, lane i to `to` + 16 i.  (Written out: in front of the transposing reads the compiler waits for
+// all copies that it knows of.  Nothing is loaded into registers; every wait for these copies is written out too.)
+__device__ __forceinline__ void copy16_bounded(__amdgpu_buffer_rsrc_t from, uint32_t offset, char* to)
+{
+    const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)to);
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(at), "v"(offset), "s"(from) : "memory", "m0");
+}
+
 template <typename T, typename TO, int FORM>
 __global__ __launch_bounds__(512, 2) void product_tiles_kernel(Product p, int tiles_m, int tiles_n, int tiles, int per_xcd)
 {
     typedef typename AccOf<T>::type Acc;
     constexpr bool GATED = FORM == kGated;
-    constexpr int EB = (int)sizeof(T);
-    constexpr int COLS = GATED ? kTileN / 2 : kTileN;  // channels of a tile
+    constexpr bool A_ACROSS = FORM == kBackWeights, B_ACROSS = FORM == kBackRows || FORM == kBackWeights;
+    constexpr int EB = (int)sizeof(T), STAGE = kStage / EB;  // rows of the sum in a stage
+    constexpr int COLS = GATED ? kTileN / 2 : kTileN;        // channels of a tile
     extern __shared__ __attribute__((aligned(16))) char smem[];  // two buffers
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -44,62 +120,106 @@ __global__ __launch_bounds__(512, 2) void product_tiles_kernel(Product p, int ti
     if (work >= tiles) return;
     const int group = work / (kGroupM * tiles_n), at = work - group * (kGroupM * tiles_n);
     const int high = min(kGroupM, tiles_m - group * kGroupM);
-    const int64_t m0 = (int64_t)(group * kGroupM + at % high) * kTileM;
+    int tile_m = group * kGroupM + at % high;
+    if constexpr (FORM == kBackWeights) {  // the second weight's tiles are behind the first's
+        const int one = tiles_m / 2;
+        if (tile_m >= one) {
+            tile_m -= one;
+            p.a0 = p.a1;
+            p.y = p.y1;
+        }
+    }
+    const int64_t m0 = (int64_t)tile_m * kTileM;
     const int n0 = at / high * COLS;
 
     const int64_t lda = p.lda * EB, ldb = p.ldb * EB, row = (int64_t)p.R * EB;
-    const int S = (int)((row + kStage - 1) / kStage);
-    const int tail = (int)((row - (int64_t)(S - 1) * kStage) / 16);  // pieces of a row in the last stage
-    const Source a{(const char*)p.a0 + m0 * lda, (p.M - 1 - m0) * lda + row};
-    const Source b0{(const char*)p.b0 + n0 * ldb, (p.N - 1 - n0) * ldb + row};
-    const Source b1{(const char*)(GATED ? p.b1 : p.b0) + n0 * ldb, (p.N - 1 - n0) * ldb + row};
+    const int S1 = (p.R + STAGE - 1) / STAGE, S = FORM == kBackRows ? 2 * S1 : S1;
+    const int rest = p.R - (S1 - 1) * STAGE;  // rows of the sum in the last stage
+    auto whole = [](int64_t bytes) { return (bytes + 15) & ~(int64_t)15; };  // (dg and du, whose rows are padded)
+    auto rows_from = [&](const void* base, int64_t ld, int64_t first, int64_t rows) {
+        return Source{(const char*)base + first * ld, (rows - 1 - first) * ld + whole(row)};
+    };
+    auto columns_from = [&](const void* base, int64_t ld, int64_t first, int64_t columns) {
+        return Source{(const char*)base + first * EB, (int64_t)(p.R - 1) * ld + whole((columns - first) * EB)};
+    };
+    const Source a0 = A_ACROSS ? columns_from(p.a0, lda, m0, p.M) : rows_from(p.a0, lda, m0, p.M);
+    const Source a1 = FORM == kBackRows ? rows_from(p.a1, lda, m0, p.M) : a0;
+    const Source b0 = B_ACROSS ? columns_from(p.b0, ldb, n0, p.N) : rows_from(p.b0, ldb, n0, p.N);
+    const Source b1 = GATED ? rows_from(p.b1, ldb, n0, p.N) : FORM == kBackRows ? columns_from(p.b1, ldb, n0, p.N) : b0;
 
-    // ---- copies: a region of 128 rows is 16 instructions of 8 rows x 128 bytes, two per wave; piece k of row r lies at place k ^ (r % 8) ----
+    // ---- copies: a region is 16 instructions of 1 KB, two per wave.  By rows: 8 rows of 128 bytes, piece k of row r at place k ^ (r % 8).
+    // A lane's channel is such that its results are neighbouring channels ----
     const int sub = lane >> 3, piece = (lane & 7) ^ sub;
+    constexpr int PIECES = 8 * EB, ROWS = 64 / PIECES;  // across: pieces of a row, rows of an instruction
     uint32_t va[2], vb[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         const int rho = wave * 16 + i * 8 + sub;
-        va[i] = (uint32_t)((rho >> 6) * 128 + (rho & 63)) * (uint32_t)lda + piece * 16;
-        const int slot = rho >> 5, j = rho >> 4 & 1, r = rho & 15;
-        const int ch = GATED ? slot * 32 + 8 * (r >> 2) + 4 * j + (r & 3) : slot * 64 + 16 * (r >> 2) + 4 * j + (r & 3);
-        vb[i] = (uint32_t)ch * (uint32_t)ldb + piece * 16;
+        const int r_across = (wave * 2 + i) * ROWS + lane / PIECES, at_across = (lane % PIECES ^ Across<T>::spread(r_across)) * 16;
+        if constexpr (A_ACROSS) va[i] = (uint32_t)r_across * (uint32_t)lda + at_across;
+        else va[i] = (uint32_t)rho * (uint32_t)lda + piece * 16;
+        if constexpr (B_ACROSS) {
+            vb[i] = (uint32_t)r_across * (uint32_t)ldb + at_across;
+        } else {
+            const int slot = rho >> 5, j = rho >> 4 & 1, r = rho & 15;
+            const int ch = GATED ? slot * 32 + 8 * (r >> 2) + 4 * j + (r & 3) : slot * 64 + 16 * (r >> 2) + 4 * j + (r & 3);
+            vb[i] = (uint32_t)ch * (uint32_t)ldb + piece * 16;
+        }
     }
     // kind: 0, 1 halves of A; 2, 3 halves of B
     auto issue = [&](int stage, int kind) {
         char* to = smem + (stage & 1) * kBuffer + kind * kRegion + wave * 2048;
-        const int64_t k = (int64_t)min(stage, S - 1) * kStage;
-        const __amdgpu_buffer_rsrc_t from = kind == 0   ? a.at(k)
-                                            : kind == 1 ? a.at(k + 64 * lda)
-                                            : kind == 2 ? b0.at(k)
-                                                        : b1.at(k + (GATED ? 0 : 8 * ldb));
+        int st = min(stage, S - 1);
+        const bool second = FORM == kBackRows && st >= S1;  // uniform: the second pair of operands
+        if (second) st -= S1;
+        __amdgpu_buffer_rsrc_t from;
+        if (kind < 2) {
+            const int64_t k = A_ACROSS ? (int64_t)st * STAGE * lda : (int64_t)st * kStage;
+            from = (second ? a1 : a0).at(k + kind * (A_ACROSS ? 128 * EB : 128 * lda));
+        } else {
+            const int64_t k = B_ACROSS ? (int64_t)st * STAGE * ldb : (int64_t)st * kStage;
+            from = ((GATED ? kind == 3 : second) ? b1 : b0).at(k + (kind - 2) * (GATED ? 0 : B_ACROSS ? 128 * EB : 8 * ldb));
+        }
 #pragma unroll
         for (int i = 0; i < 2; ++i)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)(to + i * 1024), 16, kind < 2 ? va[i] : vb[i], 0, 0, 0);
+        {
+            const uint32_t offset = kind < 2 ? va[i] : vb[i];
+            if constexpr (B_ACROSS) copy16_bounded(from, offset, to + i * 1024);
+            else __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)(to + i * 1024), 16, offset, 0, 0, 0);
+        }
     };
 
     Acc acc[8][4];
 #pragma unroll
     for (int i = 0; i < 32; ++i) acc[i >> 2][i & 3] = Acc{0, 0, 0, 0};
     u32x4 af[4][2], bf[2][2][2];  // [tile][step], [half][tile][step]
-    const int at0 = c * kStage + ((q ^ (c & 7)) * 16);  // place of piece q of row c; of piece 4 + q: the same with bit 6 flipped
+    const int at0 = c * kStage + ((q ^ (c & 7)) * 16);  // by rows: place of piece q of row c; of piece 4 + q: the same with bit 6 flipped
+    int at_a[4], at_b[2];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) at_a[t] = A_ACROSS ? Across<T>::address(wm * 4 + t, c, q) : wm * 64 * kStage + t * 16 * kStage + at0;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) at_b[t] = B_ACROSS ? Across<T>::address(wn * 2 + t, c, q) : wn * 32 * kStage + t * 16 * kStage + at0;
     auto read_a = [&](int buf, int half) {
-        const char* base = smem + buf * kBuffer + half * kRegion + wm * 64 * kStage;
+        const char* base = smem + buf * kBuffer + half * kRegion;
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
-            for (int s = 0; s < 2; ++s) af[t][s] = *(const u32x4*)(base + t * 16 * kStage + (at0 ^ (s * 64)));
+            for (int s = 0; s < 2; ++s) {
+                if constexpr (A_ACROSS) af[t][s] = Across<T>::read(base + at_a[t] + s * (kRegion / 2));
+                else af[t][s] = *(const u32x4*)(base + (at_a[t] ^ (s * 64)));
+            }
     };
     auto read_b = [&](int buf, int half) {
-        const char* base = smem + buf * kBuffer + (2 + half) * kRegion + wn * 32 * kStage;
+        const char* base = smem + buf * kBuffer + (2 + half) * kRegion;
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
-            for (int s = 0; s < 2; ++s) bf[half][t][s] = *(const u32x4*)(base + t * 16 * kStage + (at0 ^ (s * 64)));
+            for (int s = 0; s < 2; ++s) {
+                if constexpr (B_ACROSS) bf[half][t][s] = Across<T>::read(base + at_b[t] + s * (kRegion / 2));
+                else bf[half][t][s] = *(const u32x4*)(base + (at_b[t] ^ (s * 64)));
+            }
     };
-    auto clear_past = [&](u32x4& f, int s) {
-        if (4 * s + q >= tail) f = u32x4{0u, 0u, 0u, 0u};
-    };
+    auto clear_past = [&](u32x4& f, int s) { keep_first<T>(f, rest - (4 * s + q) * (16 / EB)); };
     auto multiply = [&](int ma, int nb) {
         __builtin_amdgcn_s_setprio(1);
 #pragma unroll
@@ -125,12 +245,14 @@ __global__ __launch_bounds__(512, 2) void product_tiles_kernel(Product p, int ti
     // one stage: four quadrants of the wave's tile
     auto stage_of = [&](int s, auto first) {
         constexpr int X = decltype(first)::value;  // the half of B whose operands are there already
-        const bool part = s == S - 1 && tail < 8;  // uniform: the rows end in this stage
+        const bool part = rest < STAGE && (s == S - 1 || (FORM == kBackRows && s == S1 - 1));  // uniform: the sum ends in this stage
         const int buf = X;  // (stage parity)
         read_a(buf, 0);
         issue(s + 1, 1);
         landed();
-        __builtin_amdgcn_s_waitcnt(0xc87f);  // lgkmcnt(8): and the reads in front of this stage's
+        // and the reads in front of this stage's (lgkmcnt: those of read_a may be under way; 15 would be no wait)
+        constexpr int NEW = A_ACROSS ? 8 * Across<T>::kReads : 8;
+        __builtin_amdgcn_s_waitcnt(0xc07f | (NEW < 14 ? NEW : 14) << 8);
         meet();
         if (part) {
 #pragma unroll
@@ -185,22 +307,25 @@ __global__ __launch_bounds__(512, 2) void product_tiles_kernel(Product p, int ti
     if (!wm) meet();
     __builtin_amdgcn_s_waitcnt(0x0f70);  // the surplus copies have landed: LDS may be given away
 
-    // ---- results: a lane holds 16 neighbouring channels (gated: 8 of each projection) of eight rows ----
-    constexpr int RUN = GATED ? 8 : 16;
-    const int n = n0 + wn * (GATED ? 32 : 64) + RUN * q;
-    if (n >= p.N) return;
-    const RunOutput<FORM, T, TO, RUN> out(p, n);
+    // ---- results: a lane holds 16 neighbouring channels (gated: 8 of each projection; across: four times 4) of eight rows ----
+    constexpr int RUN = GATED ? 8 : B_ACROSS ? 4 : 16, RUNS = B_ACROSS ? 4 : 1;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int64_t m = m0 + wm * 128 + i * 16 + c;
-        if (m >= p.M) continue;
-        Acc first[RUN / 4], second[RUN / 4];
+    for (int u = 0; u < RUNS; ++u) {
+        const int n = n0 + (GATED ? wn * 32 : B_ACROSS ? (u >> 1) * 128 + wn * 32 + (u & 1) * 16 : wn * 64) + RUN * q;
+        if (n >= p.N) continue;
+        const RunOutput<FORM, T, TO, RUN> out(p, n);
 #pragma unroll
-        for (int t = 0; t < RUN / 4; ++t) {
-            first[t] = acc[i][t];
-            second[t] = acc[i][GATED ? 2 + t : t];
+        for (int i = 0; i < 8; ++i) {
+            const int64_t m = m0 + (i >> 2) * 128 + wm * 64 + (i & 3) * 16 + c;
+            if (m >= p.M) continue;
+            Acc first[RUN / 4], second[RUN / 4];
+#pragma unroll
+            for (int t = 0; t < RUN / 4; ++t) {
+                first[t] = acc[i][u + t];
+                second[t] = acc[i][GATED ? 2 + t : u + t];
+            }
+            out.store(p, m, first, second);
         }
-        out.store(p, m, first, second);
     }
 }
 
@@ -212,7 +337,7 @@ template <typename T, typename TO, int FORM> rtoss_status launch(const Product& 
     if (rtoss_status st = current_device(&dev)) return st;
     const auto kernel = product_tiles_kernel<T, TO, FORM>;
     if (rtoss_status st = ensure_dynamic_lds((const void*)kernel, 2 * kBuffer, once, dev.device, "LDS of a product")) return st;
-    const int tiles_m = (int)(((int64_t)p.M + kTileM - 1) / kTileM), tiles_n = (p.N + COLS - 1) / COLS;
+    const int tiles_m = (int)(((int64_t)p.M + kTileM - 1) / kTileM) * (FORM == kBackWeights ? 2 : 1), tiles_n = (p.N + COLS - 1) / COLS;
     const int64_t tiles = (int64_t)tiles_m * tiles_n;
     const int64_t per_xcd = (tiles + 7) / 8;
     kernel<<<(unsigned)(per_xcd * 8), 512, 2 * kBuffer, s>>>(p, tiles_m, tiles_n, (int)tiles, (int)per_xcd);
@@ -221,31 +346,42 @@ template <typename T, typename TO, int FORM> rtoss_status launch(const Product& 
 
 }  // namespace
 
-bool product_pieces_ok(const Product& p, int eb, bool two)
+bool product_pieces_ok(ProductForm form, const Product& p, int eb)
 {
-    const uintptr_t all = (uintptr_t)p.a0 | (uintptr_t)p.b0 | (two ? (uintptr_t)p.b1 : 0);
-    // (a tile's rows are 32-bit offsets from its first)
-    return all % 16 == 0 && p.lda * eb % 16 == 0 && p.ldb * eb % 16 == 0 && (int64_t)p.R * eb % 16 == 0 && p.R > 0 && p.lda * eb <= 1 << 23 &&
-           p.ldb * eb <= 1 << 23;
+    const bool a_across = form == kBackWeights, b_across = a_across || form == kBackRows;
+    // (a tile's rows and a stage's are 32-bit offsets from its first)
+    const auto whole = [&](const void* q, int64_t ld) { return (uintptr_t)q % 16 == 0 && ld * eb % 16 == 0 && ld * eb <= 1 << 23; };
+    if (!whole(p.a0, p.lda) || !whole(p.b0, p.ldb)) return false;
+    if (form >= kBackRows && !whole(p.a1, p.lda)) return false;
+    if ((form == kGated || form == kBackRows) && !whole(p.b1, p.ldb)) return false;
+    // rows end with a whole piece; those of dg and du are padded to one
+    return p.R > 0 && (b_across ? (int64_t)p.N * eb % 16 == 0 : (int64_t)p.R * eb % 16 == 0);
 }
 
 bool product_tiles_ok(ProductForm form, bool bits8, rtoss_dtype out, const Product& p)
 {
-    if (form != kScaled && form != kGated) return false;
-    if (!product_pieces_ok(p, bits8 ? 1 : elem_bytes(out), form == kGated)) return false;
+    if (!product_pieces_ok(form, p, bits8 ? 1 : elem_bytes(out))) return false;
     const int cols = form == kGated ? kTileN / 2 : kTileN;
-    return (((int64_t)p.M + kTileM - 1) / kTileM) * ((p.N + cols - 1) / cols) <= kMaxGridGroups / 2;
+    return (((int64_t)p.M + kTileM - 1) / kTileM) * ((p.N + cols - 1) / cols) <= kMaxGridGroups / 4;
 }
+
+namespace {
+template <typename T> rtoss_status launch_form(ProductForm form, const Product& p, hipStream_t s)
+{
+    return form == kGated ? launch<T, T, kGated>(p, s) : form == kBackRows ? launch<T, T, kBackRows>(p, s) : launch<T, T, kBackWeights>(p, s);
+}
+template <typename TO> rtoss_status launch_bits8(ProductForm form, const Product& p, hipStream_t s)
+{
+    return form == kScaled ? launch<int8_t, TO, kScaled>(p, s) : launch<int8_t, TO, kGated>(p, s);
+}
+}  // namespace
 
 rtoss_status launch_product_tiles(ProductForm form, bool bits8, rtoss_dtype out, const Product& p, hipStream_t s)
 {
     switch (out) {
-    case RTOSS_F32:
-        return !bits8 ? launch<float, float, kGated>(p, s) : form == kScaled ? launch<int8_t, float, kScaled>(p, s) : launch<int8_t, float, kGated>(p, s);
-    case RTOSS_F16:
-        return !bits8 ? launch<f16_t, f16_t, kGated>(p, s) : form == kScaled ? launch<int8_t, f16_t, kScaled>(p, s) : launch<int8_t, f16_t, kGated>(p, s);
-    default:
-        return !bits8 ? launch<bf16_t, bf16_t, kGated>(p, s) : form == kScaled ? launch<int8_t, bf16_t, kScaled>(p, s) : launch<int8_t, bf16_t, kGated>(p, s);
+    case RTOSS_F32: return bits8 ? launch_bits8<float>(form, p, s) : launch_form<float>(form, p, s);
+    case RTOSS_F16: return bits8 ? launch_bits8<f16_t>(form, p, s) : launch_form<f16_t>(form, p, s);
+    default: return bits8 ? launch_bits8<bf16_t>(form, p, s) : launch_form<bf16_t>(form, p, s);
     }
 }
 

@@ -142,10 +142,11 @@ rtoss_status launch_quantize_rows(const void* x, rtoss_dtype dt, int64_t M, int 
 // kScaled and kGated on 8-bit operands, kGated and the gradients on operands of the result's type (product_any.hip)
 rtoss_status launch_product_any(ProductForm form, bool bits8, rtoss_dtype out, const Product& p, hipStream_t s);
 // kScaled and kGated on whole 16-byte pieces of rows, in tiles of 256 x 256 results (product_tiles.hip)
-bool product_pieces_ok(const Product& p, int eb, bool two);
+bool product_pieces_ok(ProductForm form, const Product& p, int eb);
 bool product_tiles_ok(ProductForm form, bool bits8, rtoss_dtype out, const Product& p);
 rtoss_status launch_product_tiles(ProductForm form, bool bits8, rtoss_dtype out, const Product& p, hipStream_t s);
-// dg = dh * u * act'(g), du = dh * act(g), both plain [M][F] (gated_slopes.hip)
+// dg = dh * u * act'(g), du = dh * act(g), both [M][ldd] with zeros from column F on (gated_slopes.hip); ldd: slopes_pitch
+inline int64_t slopes_pitch(int F, rtoss_dtype dt) { return (int64_t)align_up((size_t)F, 16 / elem_bytes(dt)); }
 rtoss_status launch_gated_slopes(rtoss_dtype dt, rtoss_act act, int64_t M, int F, const void* dh, int64_t ldh, const void* gate, const void* up,
                                  void* dg, void* du, hipStream_t s);
 

@@ -79,7 +79,7 @@ rtoss_status launch_product(ProductForm form, bool bits8, rtoss_dtype out, const
     return launch_product_any(form, bits8, out, p, s);
 }
 
-size_t slopes_bytes(const rtoss_gated_desc& d) { return align_up((size_t)d.M * d.F * elem_bytes(d.dt), 256); }
+size_t slopes_bytes(const rtoss_gated_desc& d) { return align_up((size_t)d.M * slopes_pitch(d.F, d.dt) * elem_bytes(d.dt), 256); }
 
 }  // namespace
 
@@ -278,7 +278,7 @@ rtoss_status rtoss_gated_ff_backward(const rtoss_gated_desc* desc, const void* d
     Product p{};
     p.a0 = dg;
     p.a1 = du;
-    p.lda = d.F;
+    p.lda = slopes_pitch(d.F, d.dt);
     if (rows) {
         p.b0 = w_gate_dev;
         p.b1 = w_up_dev;
