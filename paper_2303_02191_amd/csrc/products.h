@@ -141,7 +141,10 @@ rtoss_status launch_quantize_rows(const void* x, rtoss_dtype dt, int64_t M, int 
                                   hipStream_t s);
 // kScaled and kGated on 8-bit operands, kGated and the gradients on operands of the result's type (product_any.hip)
 rtoss_status launch_product_any(ProductForm form, bool bits8, rtoss_dtype out, const Product& p, hipStream_t s);
-// kScaled and kGated on whole 16-byte pieces of rows, in tiles of 256 x 256 results (product_tiles.hip)
+// kScaled and kGated of few rows, of any alignment (product_few.hip)
+bool product_few_ok(ProductForm form, const Product& p);
+rtoss_status launch_product_few(ProductForm form, bool bits8, rtoss_dtype out, const Product& p, hipStream_t s);
+// every form on whole 16-byte pieces of rows, in tiles of 256 x 256 results (product_tiles.hip)
 bool product_pieces_ok(ProductForm form, const Product& p, int eb);
 bool product_tiles_ok(ProductForm form, bool bits8, rtoss_dtype out, const Product& p);
 rtoss_status launch_product_tiles(ProductForm form, bool bits8, rtoss_dtype out, const Product& p, hipStream_t s);

@@ -75,6 +75,7 @@ rtoss_status gated_desc(const rtoss_gated_desc* desc, rtoss_gated_desc* d)
 
 rtoss_status launch_product(ProductForm form, bool bits8, rtoss_dtype out, const Product& p, hipStream_t s)
 {
+    if (product_few_ok(form, p)) return launch_product_few(form, bits8, out, p, s);
     if (p.M > 128 && product_tiles_ok(form, bits8, out, p)) return launch_product_tiles(form, bits8, out, p, s);
     return launch_product_any(form, bits8, out, p, s);
 }
