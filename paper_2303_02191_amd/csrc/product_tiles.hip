@@ -27,80 +27,16 @@
 #include <algorithm>
 
 #include "product_run.h"
-#include "work_order.h"
+#include "product_tile.h"
 
 namespace rtoss {
 
 namespace {
 
 constexpr int kTileM = 256, kTileN = 256;
-constexpr int kStage = 128;                 // bytes of a row in a stage
 constexpr int kRegion = 128 * kStage;       // half of an operand's rows
 constexpr int kBuffer = 4 * kRegion;        // A half 0, A half 1, B half 0, B half 1
 constexpr int kGroupM = 4;                  // row tiles that neighbouring workgroups share
-
-__device__ __forceinline__ void fence() { asm volatile("" ::: "memory"); }
-
-// An operand's rows from some row on, as a bounded buffer: loads past the matrix give nothing.
-struct Source {
-    const char* p;
-    int64_t left;  // bytes from p to the matrix's end
-    __device__ __forceinline__ __amdgpu_buffer_rsrc_t at(int64_t offset) const
-    {
-        const int64_t n = left - offset;
-        return __builtin_amdgcn_make_buffer_rsrc((void*)(p + offset), 0, (int)(uint32_t)(n < 0 ? 0 : n > 0xfffffff0ll ? 0xfffffff0ll : n), 0x00027000);
-    }
-};
-
-// The elements r .. r+E-1 of the sum that a lane holds of a fragment, of which `valid` exist: zeros for the others.
-template <typename T> __device__ __forceinline__ void keep_first(u32x4& f, int valid)
-{
-    constexpr int E = 4 / (int)sizeof(T);  // of a word
-#pragma unroll
-    for (int d = 0; d < 4; ++d) {
-        const int have = valid - d * E;
-        const uint32_t mask = have >= E ? ~0u : have <= 0 ? 0u : (1u << (have * 8 * (int)sizeof(T) & 31)) - 1;
-        f[d] &= mask;
-    }
-}
-
-// Reads of an operand that lies across: [rows of the sum][128 columns].
-template <typename T> struct Across {
-    static constexpr int kRowBytes = 128 * (int)sizeof(T);  // (a region: 64 rows of a 16-bit type, 32 of fp32)
-    static constexpr int kReads = sizeof(T) == 4 ? 4 : 2;   // per fragment
-    // place of the 16-byte piece `piece` of row r
-    static __device__ __forceinline__ int spread(int r) { return sizeof(T) == 4 ? (r >> 2 & 3) << 2 : ((r & 3) | (r >> 1 & 4)) << 1; }
-    // a lane's address of the fragment of columns 16 t .. 16 t + 15 in step 0
-    static __device__ __forceinline__ int address(int t, int c, int q)
-    {
-        if constexpr (sizeof(T) == 4) return 4 * q * kRowBytes + ((4 * t ^ spread(4 * q)) * 16) + 4 * c;
-        const int r = 8 * q + (c >> 2);
-        return r * kRowBytes + ((2 * t ^ spread(r)) * 16) + (c & 3) * 8;
-    }
-    static __device__ __forceinline__ u32x4 read(const char* at)  // + step * (half a region)
-    {
-        u32x4 f;
-        if constexpr (sizeof(T) == 4) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) f[e] = *(const uint32_t*)(at + e * kRowBytes);
-        } else {
-            typedef short s4 __attribute__((ext_vector_type(4)));
-            typedef __attribute__((address_space(3))) s4* Lds;
-            const uint2 lo = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)at));
-            const uint2 hi = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(at + 4 * kRowBytes)));
-            f = u32x4{lo.x, lo.y, hi.x, hi.y};
-        }
-        return f;
-    }
-};
-
-// 16 bytes a lane from a bounded buffer to LDS, lane i to `to` + 16 i.  (Written out: in front of the transposing reads the compiler waits for
-// all copies that it knows of.  Nothing is loaded into registers; every wait for these copies is written out too.)
-__device__ __forceinline__ void copy16_bounded(__amdgpu_buffer_rsrc_t from, uint32_t offset, char* to)
-{
-    const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)to);
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(at), "v"(offset), "s"(from) : "memory", "m0");
-}
 
 template <typename T, typename TO, int FORM>
 __global__ __launch_bounds__(512, 2) void product_tiles_kernel(Product p, int tiles_m, int tiles_n, int tiles, int per_xcd)
@@ -150,12 +86,12 @@ __global__ __launch_bounds__(512, 2) void product_tiles_kernel(Product p, int ti
     // ---- copies: a region is 16 instructions of 1 KB, two per wave.  By rows: 8 rows of 128 bytes, piece k of row r at place k ^ (r % 8).
     // A lane's channel is such that its results are neighbouring channels ----
     const int sub = lane >> 3, piece = (lane & 7) ^ sub;
-    constexpr int PIECES = 8 * EB, ROWS = 64 / PIECES;  // across: pieces of a row, rows of an instruction
+    constexpr int PIECES = Across<T, 128>::kPieces, ROWS = Across<T, 128>::kCopyRows;
     uint32_t va[2], vb[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         const int rho = wave * 16 + i * 8 + sub;
-        const int r_across = (wave * 2 + i) * ROWS + lane / PIECES, at_across = (lane % PIECES ^ Across<T>::spread(r_across)) * 16;
+        const int r_across = (wave * 2 + i) * ROWS + lane / PIECES, at_across = (lane % PIECES ^ Across<T, 128>::spread(r_across)) * 16;
         if constexpr (A_ACROSS) va[i] = (uint32_t)r_across * (uint32_t)lda + at_across;
         else va[i] = (uint32_t)rho * (uint32_t)lda + piece * 16;
         if constexpr (B_ACROSS) {
@@ -184,7 +120,7 @@ __global__ __launch_bounds__(512, 2) void product_tiles_kernel(Product p, int ti
         for (int i = 0; i < 2; ++i)
         {
             const uint32_t offset = kind < 2 ? va[i] : vb[i];
-            if constexpr (B_ACROSS) copy16_bounded(from, offset, to + i * 1024);
+            if constexpr (B_ACROSS) copy16_bounded(from, offset, __builtin_amdgcn_readfirstlane(lds_offset(to + i * 1024)));
             else __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)(to + i * 1024), 16, offset, 0, 0, 0);
         }
     };
@@ -192,42 +128,43 @@ __global__ __launch_bounds__(512, 2) void product_tiles_kernel(Product p, int ti
     Acc acc[8][4];
 #pragma unroll
     for (int i = 0; i < 32; ++i) acc[i >> 2][i & 3] = Acc{0, 0, 0, 0};
-    u32x4 af[4][2], bf[2][2][2];  // [tile][step], [half][tile][step]
+    u32x4 af[4][2], bf[4][2];  // [tile][step]
     const int at0 = c * kStage + ((q ^ (c & 7)) * 16);  // by rows: place of piece q of row c; of piece 4 + q: the same with bit 6 flipped
     int at_a[4], at_b[2];
 #pragma unroll
-    for (int t = 0; t < 4; ++t) at_a[t] = A_ACROSS ? Across<T>::address(wm * 4 + t, c, q) : wm * 64 * kStage + t * 16 * kStage + at0;
+    for (int t = 0; t < 4; ++t) at_a[t] = A_ACROSS ? Across<T, 128>::address(wm * 4 + t, c, q) : wm * 64 * kStage + t * 16 * kStage + at0;
 #pragma unroll
-    for (int t = 0; t < 2; ++t) at_b[t] = B_ACROSS ? Across<T>::address(wn * 2 + t, c, q) : wn * 32 * kStage + t * 16 * kStage + at0;
+    for (int t = 0; t < 2; ++t) at_b[t] = B_ACROSS ? Across<T, 128>::address(wn * 2 + t, c, q) : wn * 32 * kStage + t * 16 * kStage + at0;
     auto read_a = [&](int buf, int half) {
         const char* base = smem + buf * kBuffer + half * kRegion;
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
-                if constexpr (A_ACROSS) af[t][s] = Across<T>::read(base + at_a[t] + s * (kRegion / 2));
+                if constexpr (A_ACROSS) af[t][s] = Across<T, 128>::read(base + at_a[t] + s * (kRegion / 2));
                 else af[t][s] = *(const u32x4*)(base + (at_a[t] ^ (s * 64)));
             }
     };
-    auto read_b = [&](int buf, int half) {
-        const char* base = smem + buf * kBuffer + (2 + half) * kRegion;
+    auto read_b = [&](int buf) {
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
+        for (int t = 0; t < 4; ++t) {
+            const char* base = smem + buf * kBuffer + (2 + (t >> 1)) * kRegion;
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
-                if constexpr (B_ACROSS) bf[half][t][s] = Across<T>::read(base + at_b[t] + s * (kRegion / 2));
-                else bf[half][t][s] = *(const u32x4*)(base + (at_b[t] ^ (s * 64)));
+                if constexpr (B_ACROSS) bf[t][s] = Across<T, 128>::read(base + at_b[t & 1] + s * (kRegion / 2));
+                else bf[t][s] = *(const u32x4*)(base + (at_b[t & 1] ^ (s * 64)));
             }
+        }
     };
     auto clear_past = [&](u32x4& f, int s) { keep_first<T>(f, rest - (4 * s + q) * (16 / EB)); };
-    auto multiply = [&](int ma, int nb) {
+    auto multiply = [&](int ma) {
         __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int s = 0; s < 2; ++s)
 #pragma unroll
             for (int t = 0; t < 4; ++t)
 #pragma unroll
-                for (int u = 0; u < 2; ++u) acc[ma * 4 + t][nb * 2 + u] = Mma16<T>::mma(bf[nb][u][s], af[t][s], acc[ma * 4 + t][nb * 2 + u]);
+                for (int u = 0; u < 4; ++u) acc[ma * 4 + t][u] = Mma16<T>::mma(bf[u][s], af[t][s], acc[ma * 4 + t][u]);
         __builtin_amdgcn_s_setprio(0);
     };
     auto meet = [&] {
@@ -237,72 +174,38 @@ __global__ __launch_bounds__(512, 2) void product_tiles_kernel(Product p, int ti
         __builtin_amdgcn_sched_barrier(0);
         fence();
     };
-    constexpr int kWait = 0x0f70 | 10;  // vmcnt(10): the copies of all but the five newest regions have landed
-    auto landed = [&] {
+    auto landed = [&] {  // vmcnt(8): the copies of all but the four newest regions; lgkmcnt(0): operands
         fence();
-        __builtin_amdgcn_s_waitcnt(kWait);
+        __builtin_amdgcn_s_waitcnt(0x0070 | 8);
     };
-    // one stage: four quadrants of the wave's tile
-    auto stage_of = [&](int s, auto first) {
-        constexpr int X = decltype(first)::value;  // the half of B whose operands are there already
-        const bool part = rest < STAGE && (s == S - 1 || (FORM == kBackRows && s == S1 - 1));  // uniform: the sum ends in this stage
-        const int buf = X;  // (stage parity)
-        read_a(buf, 0);
-        issue(s + 1, 1);
-        landed();
-        // and the reads in front of this stage's (lgkmcnt: those of read_a may be under way; 15 would be no wait)
-        constexpr int NEW = A_ACROSS ? 8 * Across<T>::kReads : 8;
-        __builtin_amdgcn_s_waitcnt(0xc07f | (NEW < 14 ? NEW : 14) << 8);
-        meet();
-        if (part) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) clear_past(af[i >> 1][i & 1], i & 1);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) clear_past(bf[X][i >> 1][i & 1], i & 1);
-        }
-        multiply(0, X);
-        meet();
-
-        read_b(buf, 1 - X);
-        issue(s + 2, 2 + X);
-        landed();
-        meet();
-        if (part) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) clear_past(bf[1 - X][i >> 1][i & 1], i & 1);
-        }
-        multiply(0, 1 - X);
-        meet();
-
-        read_a(buf, 1);
-        issue(s + 2, 0);
-        landed();
-        meet();
-        if (part) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) clear_past(af[i >> 1][i & 1], i & 1);
-        }
-        multiply(1, 1 - X);
-        meet();
-
-        read_b(1 - buf, 1 - X);  // (of the next stage; behind the last one of something that nobody uses)
-        issue(s + 2, 3 - X);
-        landed();
-        meet();
-        multiply(1, X);
-        meet();
-    };
-
-    issue(0, 2), issue(0, 0), issue(0, 3), issue(0, 1), issue(1, 3), issue(1, 0), issue(1, 2);
+    issue(0, 2), issue(0, 3), issue(0, 0), issue(0, 1), issue(1, 2), issue(1, 3), issue(1, 0);
     landed();
     meet();
-    read_b(0, 0);
-    if (wm) meet();  // the waves of one half are half a quadrant behind the others'
-    for (int s = 0;;) {
-        stage_of(s, std::integral_constant<int, 0>{});
-        if (++s == S) break;
-        stage_of(s, std::integral_constant<int, 1>{});
-        if (++s == S) break;
+    if (wm) meet();  // the waves of one half are a part behind the others'
+    for (int s = 0; s < S; ++s) {
+        const bool part = rest < STAGE && (s == S - 1 || (FORM == kBackRows && s == S1 - 1));  // uniform: the sum ends in this stage
+        read_b(s & 1);
+        read_a(s & 1, 0);
+        issue(s + 1, 1);
+        landed();
+        meet();
+        if (part) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) clear_past(af[i >> 1][i & 1], i & 1), clear_past(bf[i >> 1][i & 1], i & 1);
+        }
+        multiply(0);
+        meet();
+
+        read_a(s & 1, 1);
+        issue(s + 2, 2), issue(s + 2, 3), issue(s + 2, 0);
+        landed();
+        meet();
+        if (part) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) clear_past(af[i >> 1][i & 1], i & 1);
+        }
+        multiply(1);
+        meet();
     }
     if (!wm) meet();
     __builtin_amdgcn_s_waitcnt(0x0f70);  // the surplus copies have landed: LDS may be given away

@@ -1,6 +1,7 @@
 // C entries of the 8-bit products and the gated feed-forward block: checks of the arguments (before any HIP call) and the choice of
 // kernels.
 #include <algorithm>
+#include <cstdlib>
 
 #include "products.h"
 
@@ -75,8 +76,14 @@ rtoss_status gated_desc(const rtoss_gated_desc* desc, rtoss_gated_desc* d)
 
 rtoss_status launch_product(ProductForm form, bool bits8, rtoss_dtype out, const Product& p, hipStream_t s)
 {
+    const char* force = getenv("RTOSS_FORCE");
+    const int f = force ? atoi(force) : -1;
+    if (f == 9 || !product_tiles_ok(form, bits8, out, p)) { if (product_few_ok(form, p) && f != 9) return launch_product_few(form, bits8, out, p, s); return launch_product_any(form, bits8, out, p, s); }
+    if ((f >= 0 && f < 3) || (f >= 4 && f < 7)) return launch_product_mid(form, bits8, out, f, p, s);
+    if (f == 7) return launch_product_slices(form, bits8, out, 0, p, s);
+    if (f == 3) return launch_product_tiles(form, bits8, out, p, s);
     if (product_few_ok(form, p)) return launch_product_few(form, bits8, out, p, s);
-    if (p.M > 128 && product_tiles_ok(form, bits8, out, p)) return launch_product_tiles(form, bits8, out, p, s);
+    if (p.M > 128) return launch_product_tiles(form, bits8, out, p, s);
     return launch_product_any(form, bits8, out, p, s);
 }
 

