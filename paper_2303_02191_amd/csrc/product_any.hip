@@ -44,7 +44,7 @@ __device__ __forceinline__ u32x4 load_piece(const T* __restrict__ p, int64_t ld,
     return out;
 }
 
-template <typename T, typename TO, int FORM> __global__ __launch_bounds__(256) void product_any_kernel(Product p, int tiles_n, int64_t tiles)
+template <typename T, typename TO, int FORM> __global__ __launch_bounds__(256, 2) void product_any_kernel(Product p, int tiles_n, int64_t tiles)
 {
     typedef typename AccOf<T>::type Acc;
     constexpr int E = 16 / (int)sizeof(T), STAGE = 4 * E;

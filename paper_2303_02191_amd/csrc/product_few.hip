@@ -33,7 +33,7 @@ template <typename T> __device__ __forceinline__ u32x4 load_past(const T* row, i
 }
 
 template <typename T, typename TO, int FORM, int MT, int WAVES, int U>
-__global__ __launch_bounds__(64 * WAVES) void product_few_kernel(Product p)
+__global__ __launch_bounds__(64 * WAVES, 2) void product_few_kernel(Product p)
 {
     typedef typename AccOf<T>::type Acc;
     constexpr int SUMS = FORM == kGated ? 2 : 1;

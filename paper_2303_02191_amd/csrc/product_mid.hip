@@ -13,7 +13,7 @@ namespace rtoss {
 namespace {
 
 template <typename T, typename TO, int FORM, int BM, int BN, int BUFS>
-__global__ __launch_bounds__(256) void product_mid_kernel(Product p, int tiles_m, int tiles_n, int tiles, int per_xcd)
+__global__ __launch_bounds__(256, 2) void product_mid_kernel(Product p, int tiles_m, int tiles_n, int tiles, int per_xcd)
 {
     typedef typename AccOf<T>::type Acc;
     constexpr bool GATED = FORM == kGated;

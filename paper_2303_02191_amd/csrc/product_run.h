@@ -74,7 +74,10 @@ template <int FORM, typename T, typename TO, int RUN> struct RunOutput {
     }
     __device__ __forceinline__ void store(const Product& p, int64_t m, const Acc (&first)[RUN / 4], const Acc (&second)[RUN / 4]) const
     {
-        const float sa = kScales && p.sa ? p.sa[m] : 1.f;
+        store(p, m, kScales && p.sa ? p.sa[m] : 1.f, first, second);
+    }
+    __device__ __forceinline__ void store(const Product& p, int64_t m, float sa, const Acc (&first)[RUN / 4], const Acc (&second)[RUN / 4]) const
+    {
         float v[RUN];
         values(v, first, s0, sa);
         if constexpr (FORM == kScaled) {

@@ -1,8 +1,9 @@
 // Products of whole 16-byte pieces whose results are few tiles: the sum split over the waves of a workgroup.
 //
-// A workgroup owns BM x BN results, and each of its four waves all of them for every fourth stage of 128 bytes of the sum, through a ring
-// of its own in LDS: no barrier before the sums are joined, and an operand is read from LDS once, where waves that share a stage would
-// read it twice (64 x 64 results by waves of 32 x 32: 48 KB of LDS a stage, here 32).  Operands lie in LDS as in product_tiles.hip.
+// A workgroup owns 64 x 64 results, and each of its eight waves all of them for every eighth stage of 128 bytes of the sum, through 16 KB of
+// its own in LDS: no barrier before the sums are joined, and an operand is read from LDS once, where waves that share a stage would
+// read it twice (waves of 32 x 32: 48 KB of LDS a stage, here 32).  Of the two waves of a SIMD one multiplies while the other waits for its
+// copies.  Operands lie in LDS as in product_tiles.hip.
 // Bound: the copies, 64 bytes a cycle and CU.
 #include <algorithm>
 
@@ -13,8 +14,52 @@ namespace rtoss {
 
 namespace {
 
-template <typename T, typename TO, int FORM, int BM, int BN, int BUFS>
-__global__ __launch_bounds__(256) void product_slices_kernel(Product p, int tiles_m, int tiles_n, int tiles, int per_xcd)
+constexpr int kWaves = 8;
+constexpr int BM = 64, BN = 64;  // results of a workgroup
+
+// How rows lie in memory, and a stage comes into LDS:
+//   kWhole  pieces of 16 bytes start at multiples of 16 bytes: copies
+//   kWords  ... at multiples of 4: through registers
+//   kBytes  ... anywhere: through registers, with the word behind (a load of 16 bytes that is not aligned to a word takes 64 cycles instead of 16)
+enum Rows { kWhole = 0, kWords, kBytes };
+
+// 16 bytes at p; kBytes: in two parts
+template <int ROWS> struct Piece {
+    u32x4 v;
+    uint32_t behind;
+    __device__ __forceinline__ void load(const char* p)
+    {
+        if constexpr (ROWS == kBytes) {
+            const uint32_t shift = (uint32_t)(uintptr_t)p & 3;
+            const char* word = p - shift;
+            v = *(const __attribute__((aligned(4))) u32x4*)word;
+            behind = *(const uint32_t*)(word + (shift ? 16 : 12));  // (only words that hold a byte of the piece)
+        } else {
+            __builtin_memcpy(&v, __builtin_assume_aligned(p, 4), 16);
+        }
+    }
+    // of which only `bytes` exist, at least one: words past the last of them repeat it
+    __device__ __forceinline__ void load_part(const char* p, int bytes)
+    {
+        const uint32_t shift = ROWS == kBytes ? (uint32_t)(uintptr_t)p & 3 : 0;
+        const uint32_t* word = (const uint32_t*)(p - shift);
+        const int last = (min(bytes, 16) + (int)shift - 1) >> 2;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) v[w] = word[min(w, last)];
+        if constexpr (ROWS == kBytes) behind = word[last];
+    }
+    __device__ __forceinline__ u32x4 value(uint32_t shift) const
+    {
+        if constexpr (ROWS == kBytes) {
+            return u32x4{__builtin_amdgcn_alignbyte(v[1], v[0], shift), __builtin_amdgcn_alignbyte(v[2], v[1], shift),
+                         __builtin_amdgcn_alignbyte(v[3], v[2], shift), __builtin_amdgcn_alignbyte(behind, v[3], shift)};
+        } else {
+            return v;
+        }
+    }
+};
+template <typename T, typename TO, int FORM, int ROWS>
+__global__ __launch_bounds__(64 * kWaves, 2) void product_slices_kernel(Product p, int tiles_m, int tiles_n, int tiles, int per_xcd)
 {
     typedef typename AccOf<T>::type Acc;
     constexpr bool GATED = FORM == kGated;
@@ -22,7 +67,6 @@ __global__ __launch_bounds__(256) void product_slices_kernel(Product p, int tile
     constexpr int EB = (int)sizeof(T), STAGE = kStage / EB;  // rows of the sum in a stage
     constexpr int COLS = GATED ? BN / 2 : BN;                // channels of a tile
     constexpr int MT = BM / 16, NT = BN / 16;                // 16 x 16 tiles
-    static_assert(MT <= 4 && 4 % MT == 0, "the four waves share the output stage");
     constexpr int A_BYTES = BM * kStage, B_BYTES = BN * kStage, BUFFER = A_BYTES + B_BYTES;
     constexpr int A_COPIES = BM / 8, B_COPIES = BN / 8;      // instructions of a stage
     extern __shared__ __attribute__((aligned(16))) char smem[];
@@ -61,7 +105,7 @@ __global__ __launch_bounds__(256) void product_slices_kernel(Product p, int tile
     const Source b1 = GATED ? rows_from(p.b1, ldb, n0, p.N) : FORM == kBackRows ? columns_from(p.b1, ldb, n0, p.N) : b0;
 
     // ---- copies; a lane's channel is such that its results are neighbouring channels.  Gated: the second half of B's rows are w_up's ----
-    typedef Across<T, BM < 64 ? 64 : BM> AcrossA;
+    typedef Across<T, BM> AcrossA;
     typedef Across<T, BN> AcrossB;
     const int sub = lane >> 3, piece = (lane & 7) ^ sub;
     uint32_t va[A_COPIES], vb[B_COPIES];
@@ -87,21 +131,27 @@ __global__ __launch_bounds__(256) void product_slices_kernel(Product p, int tile
             vb[i] = (uint32_t)(4 * TILES * (r >> 2) + 4 * t + (r & 3)) * (uint32_t)ldb + piece * 16;
         }
     }
-    char* const ring = smem + wave * (BUFS * BUFFER);
-    const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_offset(smem)) + wave * (BUFS * BUFFER);
-    auto issue = [&](int stage, int buf) {
-        const uint32_t to = lds0 + buf * BUFFER;
-        int st = min(stage, S - 1);
+    char* const own = smem + wave * BUFFER;
+    const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_offset(smem)) + wave * BUFFER;
+    struct From {
+        __amdgpu_buffer_rsrc_t a, b, up;
+    };
+    auto source = [&](int stage) {
+        int st = stage;
         const bool second = FORM == kBackRows && st >= S1;  // uniform: the second pair of operands
         if (second) st -= S1;
-        const __amdgpu_buffer_rsrc_t from_a = (second ? a1 : a0).at(A_ACROSS ? (int64_t)st * STAGE * lda : (int64_t)st * kStage);
         const int64_t kb = B_ACROSS ? (int64_t)st * STAGE * ldb : (int64_t)st * kStage;
-        const __amdgpu_buffer_rsrc_t from_b = (second ? b1 : b0).at(kb);
-        const __amdgpu_buffer_rsrc_t from_up = GATED ? b1.at(kb) : from_b;
-#pragma unroll
-        for (int i = 0; i < A_COPIES; ++i) copy16_bounded(from_a, va[i], to + i * 1024);
-#pragma unroll
-        for (int i = 0; i < B_COPIES; ++i) copy16_bounded(GATED && i >= B_COPIES / 2 ? from_up : from_b, vb[i], to + A_BYTES + i * 1024);
+        From f;
+        f.a = (second ? a1 : a0).at(A_ACROSS ? (int64_t)st * STAGE * lda : (int64_t)st * kStage);
+        f.b = (second ? b1 : b0).at(kb);
+        f.up = GATED ? b1.at(kb) : f.b;
+        return f;
+    };
+    constexpr int PIECES = A_COPIES + B_COPIES;
+    auto copy = [&](const From& f, uint32_t to, auto which) {
+        constexpr int I = decltype(which)::value;
+        if constexpr (I < A_COPIES) copy16_bounded(f.a, va[I], to + I * 1024);
+        else copy16_bounded(GATED && I - A_COPIES >= B_COPIES / 2 ? f.up : f.b, vb[I - A_COPIES], to + A_BYTES + (I - A_COPIES) * 1024);
     };
 
     Acc acc[MT][NT];
@@ -114,18 +164,19 @@ __global__ __launch_bounds__(256) void product_slices_kernel(Product p, int tile
     for (int t = 0; t < MT; ++t) at_a[t] = A_ACROSS ? AcrossA::address(t, c, q) : t * 16 * kStage + at0;
 #pragma unroll
     for (int t = 0; t < NT; ++t) at_b[t] = A_BYTES + (B_ACROSS ? AcrossB::address(t, c, q) : t * 16 * kStage + at0);
-    constexpr int PER_STAGE = A_COPIES + B_COPIES, COPIES = (BUFS - 1) * PER_STAGE;  // (of the stages behind)
-    static_assert(COPIES < 64, "the counter's range");
-    const int mine = (S - wave + 3) / 4;  // stages wave, wave + 4, ...
+    // ---- what the output stage reads, before the sum: wave w of eight stores row tile w / 2, half of its channels ----
+    const int row_tile = wave >> 1, half = wave & 1;
+    const int64_t m = m0 + row_tile * 16 + c;
+    // a lane's channels: 8 neighbouring ones; gated: 4 of each projection; across: 4 of each of two tiles
+    constexpr int RUN = GATED || B_ACROSS ? 4 : 8, RUNS = B_ACROSS ? 2 : 1;
+    int n_out[RUNS];
 #pragma unroll
-    for (int i = 0; i < BUFS; ++i) issue(wave + 4 * i, i);
-    int buf = 0;
-    for (int i = 0; i < mine; ++i) {
-        const int s = wave + 4 * i;
-        fence();
-        __builtin_amdgcn_s_waitcnt(0x0f70 | (COPIES & 15) | (COPIES >> 4) << 14);
-        fence();
-        const char* base = ring + buf * BUFFER;
+    for (int u = 0; u < RUNS; ++u) n_out[u] = n0 + (B_ACROSS ? (2 * half + u) * 16 + 4 * q : GATED ? 8 * q + 4 * half : 16 * q + 8 * half);
+    typedef RunOutput<FORM, T, TO, RUN> Output;
+    const Output out(p, min(n_out[0], p.N - 1));  // (across: it holds nothing but the place)
+    const float sa = Output::kScales && p.sa ? p.sa[min(m, (int64_t)p.M - 1)] : 1.f;
+
+    auto read_and_multiply = [&](const char* base, int s, auto&& then) {
         u32x4 af[2][MT], bf[2][NT];
 #pragma unroll
         for (int step = 0; step < 2; ++step) {
@@ -140,12 +191,8 @@ __global__ __launch_bounds__(256) void product_slices_kernel(Product p, int tile
                 else bf[step][t] = *(const u32x4*)(base + (at_b[t] ^ (step * 64)));
             }
         }
-        fence();
-        __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): the buffer is free
-        fence();
-        issue(s + 4 * BUFS, buf);
-        __builtin_amdgcn_sched_barrier(0);
-        if (__builtin_expect(rest < STAGE && (s == S - 1 || (FORM == kBackRows && s == S1 - 1)), 0)) {  // uniform: the sum ends in this stage
+        then();
+        if (ROWS == kWhole && __builtin_expect(rest < STAGE && (s == S - 1 || (FORM == kBackRows && s == S1 - 1)), 0)) {  // uniform: the sum ends here
 #pragma unroll
             for (int step = 0; step < 2; ++step) {
                 const int valid = rest - (4 * step + q) * (16 / EB);
@@ -158,89 +205,176 @@ __global__ __launch_bounds__(256) void product_slices_kernel(Product p, int tile
 #pragma unroll
         for (int step = 0; step < 2; ++step)
 #pragma unroll
-            for (int m = 0; m < MT; ++m)
+            for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int n = 0; n < NT; ++n) acc[m][n] = Mma16<T>::mma(bf[step][n], af[step][m], acc[m][n]);
-        buf = buf + 1 == BUFS ? 0 : buf + 1;
+                for (int i = 0; i < MT; ++i) acc[i][n] = Mma16<T>::mma(bf[step][n], af[step][i], acc[i][n]);
+    };
+    if constexpr (ROWS == kWhole) {
+        auto issue = [&](int s) {
+            const From f = source(s);
+            static_for<PIECES>([&](auto k) { copy(f, lds0, k); });
+        };
+        if (wave < S) issue(wave);
+        for (int s = wave; s < S; s += kWaves) {
+            fence();
+            __builtin_amdgcn_s_waitcnt(0x0f70);  // the stage has landed
+            fence();
+            read_and_multiply(own, s, [&] {
+                fence();
+                __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): its place is free
+                fence();
+                if (s + kWaves < S) issue(s + kWaves);
+                __builtin_amdgcn_sched_barrier(0);
+            });
+        }
+    } else {
+        // ---- through registers: a stage is loaded while the one before is multiplied.  (One wave's LDS instructions run in their order.) ----
+        constexpr int E = 16 / EB;
+        Piece<ROWS> piece_in[PIECES];
+        // piece i of stage st: its address, and how many of its elements exist
+        auto place = [&](int i, int st, int& have) {
+            const bool second = FORM == kBackRows && st >= S1;
+            if (second) st -= S1;
+            const bool of_a = i < A_COPIES;
+            const int k = of_a ? i : i - A_COPIES;
+            const int64_t ld = of_a ? lda : ldb;
+            if (of_a ? A_ACROSS : B_ACROSS) {
+                constexpr int per_a = AcrossA::kPieces, per_b = AcrossB::kPieces;
+                const int r = of_a ? k * AcrossA::kCopyRows + lane / per_a : k * AcrossB::kCopyRows + lane / per_b;
+                const int at = (of_a ? lane % per_a ^ AcrossA::spread(r) : lane % per_b ^ AcrossB::spread(r)) * E;
+                const int64_t first = of_a ? m0 : n0, column = first + at;
+                const int64_t row_at = (int64_t)st * STAGE + r;
+                have = row_at < p.R ? (int)min((int64_t)E, (of_a ? p.M : p.N) - column) : 0;
+                const char* base = (const char*)(of_a ? p.a0 : second ? p.b1 : p.b0);
+                return base + row_at * ld + column * EB;
+            }
+            const int rho = k * 8 + sub;
+            const int r_at = st * STAGE + piece * E;
+            have = min(E, p.R - r_at);
+            if (of_a) return (const char*)(second ? p.a1 : p.a0) + min(m0 + rho, (int64_t)p.M - 1) * ld + (int64_t)r_at * EB;
+            constexpr int TILES = GATED ? NT / 2 : NT;
+            const int in = rho % COLS, t = in / 16, r = in & 15;
+            const int n = min(n0 + 4 * TILES * (r >> 2) + 4 * t + (r & 3), p.N - 1);
+            return (const char*)(GATED && rho >= COLS ? p.b1 : p.b0) + n * ld + (int64_t)r_at * EB;
+        };
+        // whether every piece of the stage is whole: uniform
+        auto inside = [&](int st) {
+            if (FORM == kBackRows && st >= S1) st -= S1;
+            return (st + 1) * (int64_t)STAGE <= p.R && (!A_ACROSS || m0 + BM <= p.M) && (!B_ACROSS || n0 + BN <= p.N);
+        };
+        auto load = [&](int st) {
+            if (inside(st)) {
+#pragma unroll
+                for (int i = 0; i < PIECES; ++i) {
+                    int have;
+                    piece_in[i].load(place(i, st, have));
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < PIECES; ++i) {
+                    int have;
+                    const char* at = place(i, st, have);
+                    const char* any = (const char*)(i < A_COPIES ? p.a0 : p.b0);
+                    piece_in[i].load_part(have > 0 ? at : any, have > 0 ? have * EB : 1);
+                }
+            }
+        };
+        auto store = [&](int st) {
+            const bool whole_stage = inside(st);
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i) {
+                int have;
+                const char* at = place(i, st, have);
+                u32x4 v = piece_in[i].value((uint32_t)(uintptr_t)at);  // (words that do not exist: other ones, cut off here)
+                if (!whole_stage) keep_first<T>(v, have);
+                *(u32x4*)(own + (i < A_COPIES ? i * 1024 : A_BYTES + (i - A_COPIES) * 1024) + lane * 16) = v;
+            }
+        };
+        if (wave < S) load(wave);
+        for (int s = wave; s < S; s += kWaves) {
+            store(s);
+            if (s + kWaves < S) load(s + kWaves);
+            fence();
+            read_and_multiply(own, s, [&] {});
+            fence();
+        }
     }
-    __builtin_amdgcn_s_waitcnt(0x0f70);  // the surplus copies have landed
 
-    // ---- join: wave w sums up and stores row tile w (of fewer row tiles: a part of its channels) ----
-    constexpr int SHARE = 4 / MT, PART = NT / SHARE;  // waves of a row tile, channel tiles of one of them
-    static_assert(NT % SHARE == 0 && (!GATED || SHARE == 1), "a wave's channels");
-    static_assert(4 * MT * NT * 1024 <= 4 * BUFS * BUFFER, "the sums must fit the rings");
-    __syncthreads();  // every ring is free
-    Acc* const joined = (Acc*)smem;  // [wave][row tile][channel tile][lane]
-#pragma unroll
-    for (int m = 0; m < MT; ++m)
-#pragma unroll
-        for (int n = 0; n < NT; ++n) joined[((wave * MT + m) * NT + n) * 64 + lane] = acc[m][n];
+    // ---- join ----
     __syncthreads();
-    const int row_tile = wave / SHARE, first_tile = wave % SHARE * PART;
-    Acc sum[PART];
+    Acc* const joined = (Acc*)smem;  // [wave][row tile][channel tile][lane]
+    static_assert(MT * NT * 1024 <= BUFFER && MT * 2 == kWaves && NT == 4, "the sums fit the waves' places");
 #pragma unroll
-    for (int t = 0; t < PART; ++t) {
-        const Acc* from = joined + (row_tile * NT + first_tile + t) * 64 + lane;
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) joined[((wave * MT + i) * NT + n) * 64 + lane] = acc[i][n];
+    __syncthreads();
+    Acc sum[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+        const Acc* from = joined + (row_tile * NT + (GATED ? 2 * t + half : 2 * half + t)) * 64 + lane;
         sum[t] = from[0];
 #pragma unroll
-        for (int w = 1; w < 4; ++w) sum[t] += from[w * MT * NT * 64];
+        for (int w = 1; w < kWaves; ++w) sum[t] += from[w * MT * NT * 64];
     }
-    const int64_t m = m0 + row_tile * 16 + c;
     if (m >= p.M) return;
-    // a lane's channels: 4 NT neighbouring ones from 4 NT q on (gated: 2 NT of each projection; across: 4 of every tile)
-    constexpr int RUN = GATED ? 2 * NT : B_ACROSS ? 4 : 4 * PART, RUNS = B_ACROSS ? PART : 1;
 #pragma unroll
     for (int u = 0; u < RUNS; ++u) {
-        const int n = n0 + (B_ACROSS ? (first_tile + u) * 16 + 4 * q : GATED ? RUN * q : 4 * NT * q + 4 * first_tile);
-        if (n >= p.N) continue;
-        const RunOutput<FORM, T, TO, RUN> out(p, n);
-        Acc first[RUN / 4], second[RUN / 4];
-#pragma unroll
-        for (int t = 0; t < RUN / 4; ++t) {
-            first[t] = sum[u + t];
-            second[t] = sum[GATED ? NT / 2 + t : u + t];
+        if (n_out[u] >= p.N) continue;
+        if constexpr (B_ACROSS) {
+            const Acc one[1] = {sum[u]};
+            Output(p, n_out[u]).store(p, m, sa, one, one);
+        } else if constexpr (GATED) {
+            const Acc first[1] = {sum[0]}, second[1] = {sum[1]};
+            out.store(p, m, sa, first, second);
+        } else {
+            out.store(p, m, sa, sum, sum);
         }
-        out.store(p, m, first, second);
     }
 }
 
-template <typename T, typename TO, int FORM, int BM, int BN, int BUFS> rtoss_status launch(const Product& p, hipStream_t s)
+template <typename T, typename TO, int FORM, int ROWS> rtoss_status launch(const Product& p, hipStream_t s)
 {
-    constexpr int COLS = FORM == kGated ? BN / 2 : BN, LDS = 4 * BUFS * (BM + BN) * kStage;
+    constexpr int COLS = FORM == kGated ? BN / 2 : BN, LDS = kWaves * (BM + BN) * kStage;
     static LaunchOnce once;
     DeviceInfo dev;
     if (rtoss_status st = current_device(&dev)) return st;
-    const auto kernel = product_slices_kernel<T, TO, FORM, BM, BN, BUFS>;
+    const auto kernel = product_slices_kernel<T, TO, FORM, ROWS>;
     if (rtoss_status st = ensure_dynamic_lds((const void*)kernel, LDS, once, dev.device, "LDS of a product")) return st;
     const int tiles_m = (int)(((int64_t)p.M + BM - 1) / BM) * (FORM == kBackWeights ? 2 : 1), tiles_n = (p.N + COLS - 1) / COLS;
     const int64_t tiles = (int64_t)tiles_m * tiles_n, per_xcd = (tiles + 7) / 8;
-    kernel<<<(unsigned)(per_xcd * 8), 256, LDS, s>>>(p, tiles_m, tiles_n, (int)tiles, (int)per_xcd);
+    kernel<<<(unsigned)(per_xcd * 8), 64 * kWaves, LDS, s>>>(p, tiles_m, tiles_n, (int)tiles, (int)per_xcd);
     return check_hip(hipGetLastError(), "product launch");
 }
 
-template <typename T, typename TO, int FORM> rtoss_status launch_tile(int tile, const Product& p, hipStream_t s)
+template <typename T, typename TO, int FORM> rtoss_status launch_rows(const Product& p, hipStream_t s)
 {
-    return launch<T, TO, FORM, 64, 64, 2>(p, s);
+    const bool a1 = FORM == kBackRows || FORM == kBackWeights, b1 = FORM == kGated || FORM == kBackRows;
+    const uintptr_t starts = (uintptr_t)p.a0 | (uintptr_t)p.b0 | (a1 ? (uintptr_t)p.a1 : 0) | (b1 ? (uintptr_t)p.b1 : 0);
+    const uintptr_t all = starts | (uintptr_t)(p.lda * (int)sizeof(T)) | (uintptr_t)(p.ldb * (int)sizeof(T));
+    if (product_pieces_ok((ProductForm)FORM, p, (int)sizeof(T))) return launch<T, TO, FORM, kWhole>(p, s);
+    if (sizeof(T) == 4 || all % 4 == 0) return launch<T, TO, FORM, kWords>(p, s);
+    if constexpr (sizeof(T) < 4) return launch<T, TO, FORM, kBytes>(p, s);
+    return RTOSS_OK;
 }
 
-template <typename T> rtoss_status launch_form(ProductForm form, int tile, const Product& p, hipStream_t s)
+template <typename T> rtoss_status launch_form(ProductForm form, const Product& p, hipStream_t s)
 {
-    return form == kGated ? launch_tile<T, T, kGated>(tile, p, s) : form == kBackRows ? launch_tile<T, T, kBackRows>(tile, p, s)
-                                                                                      : launch_tile<T, T, kBackWeights>(tile, p, s);
+    return form == kGated ? launch_rows<T, T, kGated>(p, s) : form == kBackRows ? launch_rows<T, T, kBackRows>(p, s) : launch_rows<T, T, kBackWeights>(p, s);
 }
-template <typename TO> rtoss_status launch_bits8(ProductForm form, int tile, const Product& p, hipStream_t s)
+template <typename TO> rtoss_status launch_bits8(ProductForm form, const Product& p, hipStream_t s)
 {
-    return form == kScaled ? launch_tile<int8_t, TO, kScaled>(tile, p, s) : launch_tile<int8_t, TO, kGated>(tile, p, s);
+    return form == kScaled ? launch_rows<int8_t, TO, kScaled>(p, s) : launch_rows<int8_t, TO, kGated>(p, s);
 }
 
 }  // namespace
 
-rtoss_status launch_product_slices(ProductForm form, bool bits8, rtoss_dtype out, int tile, const Product& p, hipStream_t s)
+rtoss_status launch_product_slices(ProductForm form, bool bits8, rtoss_dtype out, const Product& p, hipStream_t s)
 {
     switch (out) {
-    case RTOSS_F32: return bits8 ? launch_bits8<float>(form, tile, p, s) : launch_form<float>(form, tile, p, s);
-    case RTOSS_F16: return bits8 ? launch_bits8<f16_t>(form, tile, p, s) : launch_form<f16_t>(form, tile, p, s);
-    default: return bits8 ? launch_bits8<bf16_t>(form, tile, p, s) : launch_form<bf16_t>(form, tile, p, s);
+    case RTOSS_F32: return bits8 ? launch_bits8<float>(form, p, s) : launch_form<float>(form, p, s);
+    case RTOSS_F16: return bits8 ? launch_bits8<f16_t>(form, p, s) : launch_form<f16_t>(form, p, s);
+    default: return bits8 ? launch_bits8<bf16_t>(form, p, s) : launch_form<bf16_t>(form, p, s);
     }
 }
 

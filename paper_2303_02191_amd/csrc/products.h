@@ -151,7 +151,7 @@ rtoss_status launch_product_tiles(ProductForm form, bool bits8, rtoss_dtype out,
 // the same in small tiles, 0: 64 x 64, 1: 128 x 64, 2: 128 x 128 (product_mid.hip)
 rtoss_status launch_product_mid(ProductForm form, bool bits8, rtoss_dtype out, int tile, const Product& p, hipStream_t s);
 // ... of few tiles: the sum split over the waves of a workgroup (product_slices.hip)
-rtoss_status launch_product_slices(ProductForm form, bool bits8, rtoss_dtype out, int tile, const Product& p, hipStream_t s);
+rtoss_status launch_product_slices(ProductForm form, bool bits8, rtoss_dtype out, const Product& p, hipStream_t s);
 // dg = dh * u * act'(g), du = dh * act(g), both [M][ldd] with zeros from column F on (gated_slopes.hip); ldd: slopes_pitch
 inline int64_t slopes_pitch(int F, rtoss_dtype dt) { return (int64_t)align_up((size_t)F, 16 / elem_bytes(dt)); }
 rtoss_status launch_gated_slopes(rtoss_dtype dt, rtoss_act act, int64_t M, int F, const void* dh, int64_t ldh, const void* gate, const void* up,

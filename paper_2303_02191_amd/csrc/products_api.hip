@@ -78,9 +78,10 @@ rtoss_status launch_product(ProductForm form, bool bits8, rtoss_dtype out, const
 {
     const char* force = getenv("RTOSS_FORCE");
     const int f = force ? atoi(force) : -1;
+    if (f == 7) return launch_product_slices(form, bits8, out, p, s);
     if (f == 9 || !product_tiles_ok(form, bits8, out, p)) { if (product_few_ok(form, p) && f != 9) return launch_product_few(form, bits8, out, p, s); return launch_product_any(form, bits8, out, p, s); }
     if ((f >= 0 && f < 3) || (f >= 4 && f < 7)) return launch_product_mid(form, bits8, out, f, p, s);
-    if (f == 7) return launch_product_slices(form, bits8, out, 0, p, s);
+    if (f == 7) return launch_product_slices(form, bits8, out, p, s);
     if (f == 3) return launch_product_tiles(form, bits8, out, p, s);
     if (product_few_ok(form, p)) return launch_product_few(form, bits8, out, p, s);
     if (p.M > 128) return launch_product_tiles(form, bits8, out, p, s);
