@@ -7,6 +7,7 @@
 // Bound: the copies, 64 bytes a cycle and CU.
 #include <algorithm>
 
+#include "fp32_split.h"
 #include "product_run.h"
 #include "product_tile.h"
 
@@ -15,50 +16,8 @@ namespace rtoss {
 namespace {
 
 constexpr int kWaves = 8;
-constexpr int BM = 64, BN = 64;  // results of a workgroup
 
-// How rows lie in memory, and a stage comes into LDS:
-//   kWhole  pieces of 16 bytes start at multiples of 16 bytes: copies
-//   kWords  ... at multiples of 4: through registers
-//   kBytes  ... anywhere: through registers, with the word behind (a load of 16 bytes that is not aligned to a word takes 64 cycles instead of 16)
-enum Rows { kWhole = 0, kWords, kBytes };
-
-// 16 bytes at p; kBytes: in two parts
-template <int ROWS> struct Piece {
-    u32x4 v;
-    uint32_t behind;
-    __device__ __forceinline__ void load(const char* p)
-    {
-        if constexpr (ROWS == kBytes) {
-            const uint32_t shift = (uint32_t)(uintptr_t)p & 3;
-            const char* word = p - shift;
-            v = *(const __attribute__((aligned(4))) u32x4*)word;
-            behind = *(const uint32_t*)(word + (shift ? 16 : 12));  // (only words that hold a byte of the piece)
-        } else {
-            __builtin_memcpy(&v, __builtin_assume_aligned(p, 4), 16);
-        }
-    }
-    // of which only `bytes` exist, at least one: words past the last of them repeat it
-    __device__ __forceinline__ void load_part(const char* p, int bytes)
-    {
-        const uint32_t shift = ROWS == kBytes ? (uint32_t)(uintptr_t)p & 3 : 0;
-        const uint32_t* word = (const uint32_t*)(p - shift);
-        const int last = (min(bytes, 16) + (int)shift - 1) >> 2;
-#pragma unroll
-        for (int w = 0; w < 4; ++w) v[w] = word[min(w, last)];
-        if constexpr (ROWS == kBytes) behind = word[last];
-    }
-    __device__ __forceinline__ u32x4 value(uint32_t shift) const
-    {
-        if constexpr (ROWS == kBytes) {
-            return u32x4{__builtin_amdgcn_alignbyte(v[1], v[0], shift), __builtin_amdgcn_alignbyte(v[2], v[1], shift),
-                         __builtin_amdgcn_alignbyte(v[3], v[2], shift), __builtin_amdgcn_alignbyte(behind, v[3], shift)};
-        } else {
-            return v;
-        }
-    }
-};
-template <typename T, typename TO, int FORM, int ROWS>
+template <typename T, typename TO, int FORM, int ROWS, int BM, int BN>
 __global__ __launch_bounds__(64 * kWaves, 2) void product_slices_kernel(Product p, int tiles_m, int tiles_n, int tiles, int per_xcd)
 {
     typedef typename AccOf<T>::type Acc;
@@ -74,11 +33,14 @@ __global__ __launch_bounds__(64 * kWaves, 2) void product_slices_kernel(Product 
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c = lane & 15, q = lane >> 4;
 
-    // (XCD-contiguous, rows fastest: the weights are read once, the rows stay in the XCD's L2)
+    // XCD-contiguous, in groups of eight row tiles, rows fastest: the workgroups that run on an XCD at a time share rows and channels in its L2
     const int work = (int)(blockIdx.x % 8) * per_xcd + (int)(blockIdx.x / 8);
     if (work >= tiles) return;
-    int tile_m = work % tiles_m;
-    const int n0 = work / tiles_m * COLS;
+    constexpr int GROUP = 8;
+    const int group = work / (GROUP * tiles_n), in_group = work - group * (GROUP * tiles_n);
+    const int high = min(GROUP, tiles_m - group * GROUP);
+    int tile_m = group * GROUP + in_group % high;
+    const int n0 = in_group / high * COLS;
     if constexpr (FORM == kBackWeights) {  // the second weight's tiles are behind the first's
         const int one = tiles_m / 2;
         if (tile_m >= one) {
@@ -105,8 +67,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void product_slices_kernel(Product 
     const Source b1 = GATED ? rows_from(p.b1, ldb, n0, p.N) : FORM == kBackRows ? columns_from(p.b1, ldb, n0, p.N) : b0;
 
     // ---- copies; a lane's channel is such that its results are neighbouring channels.  Gated: the second half of B's rows are w_up's ----
-    typedef Across<T, BM> AcrossA;
-    typedef Across<T, BN> AcrossB;
+    typedef Across<T, 64> AcrossA, AcrossB;
+    static_assert((!A_ACROSS || BM == 64) && (!B_ACROSS || BN == 64), "operands that lie across");
     const int sub = lane >> 3, piece = (lane & 7) ^ sub;
     uint32_t va[A_COPIES], vb[B_COPIES];
 #pragma unroll
@@ -164,14 +126,17 @@ __global__ __launch_bounds__(64 * kWaves, 2) void product_slices_kernel(Product 
     for (int t = 0; t < MT; ++t) at_a[t] = A_ACROSS ? AcrossA::address(t, c, q) : t * 16 * kStage + at0;
 #pragma unroll
     for (int t = 0; t < NT; ++t) at_b[t] = A_BYTES + (B_ACROSS ? AcrossB::address(t, c, q) : t * 16 * kStage + at0);
-    // ---- what the output stage reads, before the sum: wave w of eight stores row tile w / 2, half of its channels ----
-    const int row_tile = wave >> 1, half = wave & 1;
+    // ---- what the output stage reads, before the sum.  Wave w stores unit w: of a row tile, PART channel tiles (gated: one of each projection)
+    constexpr int PART = NT == 1 ? 1 : 2, SHARE = NT / PART, UNITS = MT * SHARE;
+    static_assert(UNITS <= kWaves && (!GATED || NT >= 2), "a wave's share of the results");
+    const int row_tile = wave / SHARE % MT, share = wave % SHARE;
     const int64_t m = m0 + row_tile * 16 + c;
-    // a lane's channels: 8 neighbouring ones; gated: 4 of each projection; across: 4 of each of two tiles
-    constexpr int RUN = GATED || B_ACROSS ? 4 : 8, RUNS = B_ACROSS ? 2 : 1;
+    // a lane's channels: 4 PART neighbouring ones; gated: 4 of each projection; across: 4 of each tile
+    constexpr int RUN = GATED || B_ACROSS ? 4 : 4 * PART, RUNS = B_ACROSS ? PART : 1;
     int n_out[RUNS];
 #pragma unroll
-    for (int u = 0; u < RUNS; ++u) n_out[u] = n0 + (B_ACROSS ? (2 * half + u) * 16 + 4 * q : GATED ? 8 * q + 4 * half : 16 * q + 8 * half);
+    for (int u = 0; u < RUNS; ++u)
+        n_out[u] = n0 + (B_ACROSS ? (PART * share + u) * 16 + 4 * q : GATED ? 2 * NT * q + 4 * share : 4 * NT * q + 4 * PART * share);
     typedef RunOutput<FORM, T, TO, RUN> Output;
     const Output out(p, min(n_out[0], p.N - 1));  // (across: it holds nothing but the place)
     const float sa = Output::kScales && p.sa ? p.sa[min(m, (int64_t)p.M - 1)] : 1.f;
@@ -202,12 +167,27 @@ __global__ __launch_bounds__(64 * kWaves, 2) void product_slices_kernel(Product 
                 for (int t = 0; t < NT; ++t) keep_first<T>(bf[step][t], valid);
             }
         }
+        if constexpr (sizeof(T) == 4) {
+            // six products of bf16 parts (fp32_split.h), smallest first, all into one accumulator: a wave sums an eighth of the terms
+            Split8 bs[NT];
 #pragma unroll
-        for (int step = 0; step < 2; ++step)
+            for (int n = 0; n < NT; ++n) bs[n] = split8(bf[0][n], bf[1][n]);
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
+            for (int i = 0; i < MT; ++i) {
+                const Split8 as = split8(af[0][i], af[1][i]);
+                split_steps<kSplitSix>([&](auto k) {
 #pragma unroll
-                for (int i = 0; i < MT; ++i) acc[i][n] = Mma16<T>::mma(bf[step][n], af[step][i], acc[i][n]);
+                    for (int n = 0; n < NT; ++n) split_step<decltype(k)::value>(bs[n], as, acc[i][n], acc[i][n]);
+                });
+            }
+        } else {
+#pragma unroll
+            for (int step = 0; step < 2; ++step)
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int i = 0; i < MT; ++i) acc[i][n] = Mma16<T>::mma(bf[step][n], af[step][i], acc[i][n]);
+        }
     };
     if constexpr (ROWS == kWhole) {
         auto issue = [&](int s) {
@@ -303,16 +283,17 @@ __global__ __launch_bounds__(64 * kWaves, 2) void product_slices_kernel(Product 
     // ---- join ----
     __syncthreads();
     Acc* const joined = (Acc*)smem;  // [wave][row tile][channel tile][lane]
-    static_assert(MT * NT * 1024 <= BUFFER && MT * 2 == kWaves && NT == 4, "the sums fit the waves' places");
+    static_assert(MT * NT * 1024 <= BUFFER, "the sums fit the waves' places");
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
         for (int n = 0; n < NT; ++n) joined[((wave * MT + i) * NT + n) * 64 + lane] = acc[i][n];
     __syncthreads();
-    Acc sum[2];
+    if (wave >= UNITS) return;
+    Acc sum[PART];
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-        const Acc* from = joined + (row_tile * NT + (GATED ? 2 * t + half : 2 * half + t)) * 64 + lane;
+    for (int t = 0; t < PART; ++t) {
+        const Acc* from = joined + (row_tile * NT + (GATED ? NT / 2 * t + share : PART * share + t)) * 64 + lane;
         sum[t] = from[0];
 #pragma unroll
         for (int w = 1; w < kWaves; ++w) sum[t] += from[w * MT * NT * 64];
@@ -325,7 +306,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void product_slices_kernel(Product 
             const Acc one[1] = {sum[u]};
             Output(p, n_out[u]).store(p, m, sa, one, one);
         } else if constexpr (GATED) {
-            const Acc first[1] = {sum[0]}, second[1] = {sum[1]};
+            const Acc first[1] = {sum[0]}, second[1] = {sum[PART - 1]};
             out.store(p, m, sa, first, second);
         } else {
             out.store(p, m, sa, sum, sum);
@@ -333,13 +314,13 @@ __global__ __launch_bounds__(64 * kWaves, 2) void product_slices_kernel(Product 
     }
 }
 
-template <typename T, typename TO, int FORM, int ROWS> rtoss_status launch(const Product& p, hipStream_t s)
+template <typename T, typename TO, int FORM, int ROWS, int BM, int BN> rtoss_status launch(const Product& p, hipStream_t s)
 {
     constexpr int COLS = FORM == kGated ? BN / 2 : BN, LDS = kWaves * (BM + BN) * kStage;
     static LaunchOnce once;
     DeviceInfo dev;
     if (rtoss_status st = current_device(&dev)) return st;
-    const auto kernel = product_slices_kernel<T, TO, FORM, ROWS>;
+    const auto kernel = product_slices_kernel<T, TO, FORM, ROWS, BM, BN>;
     if (rtoss_status st = ensure_dynamic_lds((const void*)kernel, LDS, once, dev.device, "LDS of a product")) return st;
     const int tiles_m = (int)(((int64_t)p.M + BM - 1) / BM) * (FORM == kBackWeights ? 2 : 1), tiles_n = (p.N + COLS - 1) / COLS;
     const int64_t tiles = (int64_t)tiles_m * tiles_n, per_xcd = (tiles + 7) / 8;
@@ -347,34 +328,47 @@ template <typename T, typename TO, int FORM, int ROWS> rtoss_status launch(const
     return check_hip(hipGetLastError(), "product launch");
 }
 
-template <typename T, typename TO, int FORM> rtoss_status launch_rows(const Product& p, hipStream_t s)
+template <typename T, typename TO, int FORM, int ROWS> rtoss_status launch_tile(int tile, const Product& p, hipStream_t s)
 {
-    const bool a1 = FORM == kBackRows || FORM == kBackWeights, b1 = FORM == kGated || FORM == kBackRows;
-    const uintptr_t starts = (uintptr_t)p.a0 | (uintptr_t)p.b0 | (a1 ? (uintptr_t)p.a1 : 0) | (b1 ? (uintptr_t)p.b1 : 0);
-    const uintptr_t all = starts | (uintptr_t)(p.lda * (int)sizeof(T)) | (uintptr_t)(p.ldb * (int)sizeof(T));
-    if (product_pieces_ok((ProductForm)FORM, p, (int)sizeof(T))) return launch<T, TO, FORM, kWhole>(p, s);
-    if (sizeof(T) == 4 || all % 4 == 0) return launch<T, TO, FORM, kWords>(p, s);
-    if constexpr (sizeof(T) < 4) return launch<T, TO, FORM, kBytes>(p, s);
-    return RTOSS_OK;
+    constexpr int G = FORM == kGated ? 2 : 1;  // (rows of both weights)
+    if constexpr (FORM == kScaled || FORM == kGated) {
+        switch (tile) {
+        case 0: return launch<T, TO, FORM, ROWS, 16, 16 * G>(p, s);
+        case 1: return launch<T, TO, FORM, ROWS, 32, 16 * G>(p, s);
+        case 2: return launch<T, TO, FORM, ROWS, 32, 32 * G>(p, s);
+        case 3: return launch<T, TO, FORM, ROWS, 64, 32>(p, s);
+        }
+    }
+    return launch<T, TO, FORM, ROWS, 64, 64>(p, s);
 }
 
-template <typename T> rtoss_status launch_form(ProductForm form, const Product& p, hipStream_t s)
+template <typename T, typename TO, int FORM> rtoss_status launch_rows(int tile, const Product& p, hipStream_t s)
 {
-    return form == kGated ? launch_rows<T, T, kGated>(p, s) : form == kBackRows ? launch_rows<T, T, kBackRows>(p, s) : launch_rows<T, T, kBackWeights>(p, s);
+    switch (product_rows((ProductForm)FORM, p, (int)sizeof(T))) {
+    case kWhole: return launch_tile<T, TO, FORM, kWhole>(tile, p, s);
+    case kWords: return launch_tile<T, TO, FORM, kWords>(tile, p, s);
+    default: return launch_tile<T, TO, FORM, sizeof(T) == 4 ? kWords : kBytes>(tile, p, s);  // (elements of four bytes are words)
+    }
 }
-template <typename TO> rtoss_status launch_bits8(ProductForm form, const Product& p, hipStream_t s)
+
+template <typename T> rtoss_status launch_form(ProductForm form, int tile, const Product& p, hipStream_t s)
 {
-    return form == kScaled ? launch_rows<int8_t, TO, kScaled>(p, s) : launch_rows<int8_t, TO, kGated>(p, s);
+    return form == kGated ? launch_rows<T, T, kGated>(tile, p, s) : form == kBackRows ? launch_rows<T, T, kBackRows>(tile, p, s)
+                                                                                       : launch_rows<T, T, kBackWeights>(tile, p, s);
+}
+template <typename TO> rtoss_status launch_bits8(ProductForm form, int tile, const Product& p, hipStream_t s)
+{
+    return form == kScaled ? launch_rows<int8_t, TO, kScaled>(tile, p, s) : launch_rows<int8_t, TO, kGated>(tile, p, s);
 }
 
 }  // namespace
 
-rtoss_status launch_product_slices(ProductForm form, bool bits8, rtoss_dtype out, const Product& p, hipStream_t s)
+rtoss_status launch_product_slices(ProductForm form, bool bits8, rtoss_dtype out, int tile, const Product& p, hipStream_t s)
 {
     switch (out) {
-    case RTOSS_F32: return bits8 ? launch_bits8<float>(form, p, s) : launch_form<float>(form, p, s);
-    case RTOSS_F16: return bits8 ? launch_bits8<f16_t>(form, p, s) : launch_form<f16_t>(form, p, s);
-    default: return bits8 ? launch_bits8<bf16_t>(form, p, s) : launch_form<bf16_t>(form, p, s);
+    case RTOSS_F32: return bits8 ? launch_bits8<float>(form, tile, p, s) : launch_form<float>(form, tile, p, s);
+    case RTOSS_F16: return bits8 ? launch_bits8<f16_t>(form, tile, p, s) : launch_form<f16_t>(form, tile, p, s);
+    default: return bits8 ? launch_bits8<bf16_t>(form, tile, p, s) : launch_form<bf16_t>(form, tile, p, s);
     }
 }
 

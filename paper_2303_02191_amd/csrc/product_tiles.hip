@@ -33,23 +33,25 @@ namespace rtoss {
 
 namespace {
 
-constexpr int kTileM = 256, kTileN = 256;
-constexpr int kRegion = 128 * kStage;       // half of an operand's rows
-constexpr int kBuffer = 4 * kRegion;        // A half 0, A half 1, B half 0, B half 1
+constexpr int kTileM = 256;
+constexpr int kRegion = 128 * kStage;       // 128 rows of an operand
 constexpr int kGroupM = 4;                  // row tiles that neighbouring workgroups share
 
-template <typename T, typename TO, int FORM>
+template <typename T, typename TO, int FORM, int TILE_N, int ROWS>
 __global__ __launch_bounds__(512, 2) void product_tiles_kernel(Product p, int tiles_m, int tiles_n, int tiles, int per_xcd)
 {
     typedef typename AccOf<T>::type Acc;
     constexpr bool GATED = FORM == kGated;
     constexpr bool A_ACROSS = FORM == kBackWeights, B_ACROSS = FORM == kBackRows || FORM == kBackWeights;
     constexpr int EB = (int)sizeof(T), STAGE = kStage / EB;  // rows of the sum in a stage
-    constexpr int COLS = GATED ? kTileN / 2 : kTileN;        // channels of a tile
+    constexpr int COLS = GATED ? TILE_N / 2 : TILE_N;        // channels of a tile
+    constexpr int WN = TILE_N / 64, WM = 8 / WN, MT = 8 / WM;  // waves across channels and rows; row tiles of a wave in half of the rows
+    constexpr int B_REGIONS = TILE_N / 128, kBuffer = (2 + B_REGIONS) * kRegion;  // halves of A, then B
     extern __shared__ __attribute__((aligned(16))) char smem[];  // two buffers
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int wm = wave >> 2, wn = wave & 3;
+    const int wm = wave / WN, wn = wave % WN;
+    const bool late = wave >= 4;  // the second wave of a SIMD
     const int c = lane & 15, q = lane >> 4;
 
     const int work = (int)(blockIdx.x % 8) * per_xcd + (int)(blockIdx.x / 8);
@@ -86,23 +88,29 @@ __global__ __launch_bounds__(512, 2) void product_tiles_kernel(Product p, int ti
     // ---- copies: a region is 16 instructions of 1 KB, two per wave.  By rows: 8 rows of 128 bytes, piece k of row r at place k ^ (r % 8).
     // A lane's channel is such that its results are neighbouring channels ----
     const int sub = lane >> 3, piece = (lane & 7) ^ sub;
-    constexpr int PIECES = Across<T, 128>::kPieces, ROWS = Across<T, 128>::kCopyRows;
+    constexpr int PIECES = Across<T, 128>::kPieces, COPY_ROWS = Across<T, 128>::kCopyRows;
+    // a region's row of B -> channel of the tile (gated: runs of 8 channels a lane in 32 of a wave; otherwise of 16 in 64, of which a region
+    // has half where there are two, the second 8 channels on)
+    auto channel = [](int rho) {
+        const int r = rho & 15, tile = rho >> 4;
+        if constexpr (GATED) return (tile * 16 & COLS - 1) / 32 * 32 + 8 * (r >> 2) + 4 * (tile & 1) + (r & 3);
+        else if constexpr (B_REGIONS == 2) return (tile >> 1) * 64 + 16 * (r >> 2) + 4 * (tile & 1) + (r & 3);
+        else return (tile >> 2) * 64 + 16 * (r >> 2) + 4 * (tile & 3) + (r & 3);
+    };
     uint32_t va[2], vb[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         const int rho = wave * 16 + i * 8 + sub;
-        const int r_across = (wave * 2 + i) * ROWS + lane / PIECES, at_across = (lane % PIECES ^ Across<T, 128>::spread(r_across)) * 16;
+        const int r_across = (wave * 2 + i) * COPY_ROWS + lane / PIECES, at_across = (lane % PIECES ^ Across<T, 128>::spread(r_across)) * 16;
         if constexpr (A_ACROSS) va[i] = (uint32_t)r_across * (uint32_t)lda + at_across;
         else va[i] = (uint32_t)rho * (uint32_t)lda + piece * 16;
         if constexpr (B_ACROSS) {
             vb[i] = (uint32_t)r_across * (uint32_t)ldb + at_across;
         } else {
-            const int slot = rho >> 5, j = rho >> 4 & 1, r = rho & 15;
-            const int ch = GATED ? slot * 32 + 8 * (r >> 2) + 4 * j + (r & 3) : slot * 64 + 16 * (r >> 2) + 4 * j + (r & 3);
-            vb[i] = (uint32_t)ch * (uint32_t)ldb + piece * 16;
+            vb[i] = (uint32_t)channel(rho) * (uint32_t)ldb + piece * 16;
         }
     }
-    // kind: 0, 1 halves of A; 2, 3 halves of B
+    // kind: 0, 1 halves of A; 2, 3 regions of B.  Gated with one region: w_gate's rows, then w_up's, which are the upper waves' to copy
     auto issue = [&](int stage, int kind) {
         char* to = smem + (stage & 1) * kBuffer + kind * kRegion + wave * 2048;
         int st = min(stage, S - 1);
@@ -114,7 +122,8 @@ __global__ __launch_bounds__(512, 2) void product_tiles_kernel(Product p, int ti
             from = (second ? a1 : a0).at(k + kind * (A_ACROSS ? 128 * EB : 128 * lda));
         } else {
             const int64_t k = B_ACROSS ? (int64_t)st * STAGE * ldb : (int64_t)st * kStage;
-            from = ((GATED ? kind == 3 : second) ? b1 : b0).at(k + (kind - 2) * (GATED ? 0 : B_ACROSS ? 128 * EB : 8 * ldb));
+            const bool other = GATED ? (B_REGIONS == 2 ? kind == 3 : late) : second;
+            from = (other ? b1 : b0).at(k + (kind - 2) * (GATED ? 0 : B_ACROSS ? 128 * EB : 8 * ldb));
         }
 #pragma unroll
         for (int i = 0; i < 2; ++i)
@@ -125,20 +134,80 @@ __global__ __launch_bounds__(512, 2) void product_tiles_kernel(Product p, int ti
         }
     };
 
-    Acc acc[8][4];
+    // ---- rows that are no whole pieces: through registers, a stage's six pieces of a lane at once ----
+    constexpr int E = 16 / EB, KINDS = 2 + B_REGIONS;
+    static_assert(ROWS == kWhole || B_REGIONS == 1, "the second region's channels");
+    Piece<ROWS> piece_in[ROWS == kWhole ? 1 : 2 * KINDS];
+    // piece i of region `kind`: its address, and how many of its elements exist
+    auto place = [&](int kind, int i, int stage, int& have) {
+        int st = stage;
+        const bool second = FORM == kBackRows && st >= S1;
+        if (second) st -= S1;
+        const bool of_a = kind < 2;
+        const int64_t ld = of_a ? lda : ldb;
+        if (of_a ? A_ACROSS : B_ACROSS) {
+            const int r = (wave * 2 + i) * COPY_ROWS + lane / PIECES;
+            const int64_t row_at = (int64_t)st * STAGE + r;
+            const int64_t column = (of_a ? m0 + kind * 128 : n0) + (lane % PIECES ^ Across<T, 128>::spread(r)) * E;
+            have = row_at < p.R ? (int)min((int64_t)E, (of_a ? p.M : p.N) - column) : 0;
+            return (const char*)(of_a ? p.a0 : second ? p.b1 : p.b0) + row_at * ld + column * EB;
+        }
+        const int rho = wave * 16 + i * 8 + sub, r_at = st * STAGE + piece * E;
+        have = min(E, p.R - r_at);
+        if (of_a) return (const char*)(second ? p.a1 : p.a0) + min(m0 + kind * 128 + rho, (int64_t)p.M - 1) * ld + (int64_t)r_at * EB;
+        return (const char*)(GATED && late ? p.b1 : p.b0) + (int64_t)min(n0 + channel(rho), p.N - 1) * ld + (int64_t)r_at * EB;
+    };
+    auto inside = [&](int stage) {  // every piece of the stage is whole: uniform
+        const int st = FORM == kBackRows && stage >= S1 ? stage - S1 : stage;
+        return (st + 1) * (int64_t)STAGE <= p.R && (!A_ACROSS || m0 + kTileM <= p.M) && (!B_ACROSS || n0 + TILE_N <= p.N);
+    };
+    auto load = [&](int stage) {
+        if (inside(stage)) {
 #pragma unroll
-    for (int i = 0; i < 32; ++i) acc[i >> 2][i & 3] = Acc{0, 0, 0, 0};
-    u32x4 af[4][2], bf[4][2];  // [tile][step]
+            for (int k = 0; k < 2 * KINDS; ++k) {
+                int have;
+                piece_in[k].load(place(k / 2, k % 2, stage, have));
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < 2 * KINDS; ++k) {
+                int have;
+                const char* at = place(k / 2, k % 2, stage, have);
+                piece_in[k].load_part(have > 0 ? at : (const char*)(k < 4 ? p.a0 : p.b0), have > 0 ? have * EB : 1);
+            }
+        }
+    };
+    auto store = [&](int stage) {
+        const bool whole_stage = inside(stage);
+#pragma unroll
+        for (int k = 0; k < 2 * KINDS; ++k) {
+            int have;
+            const char* at = place(k / 2, k % 2, stage, have);
+            u32x4 v = piece_in[k].value((uint32_t)(uintptr_t)at);  // (words that do not exist: other ones, cut off here)
+            if (!whole_stage) keep_first<T>(v, have);
+            *(u32x4*)(smem + (stage & 1) * kBuffer + k / 2 * kRegion + wave * 2048 + k % 2 * 1024 + lane * 16) = v;
+        }
+    };
+
+    Acc acc[2 * MT][4];
+#pragma unroll
+    for (int i = 0; i < 8 * MT; ++i) acc[i >> 2][i & 3] = Acc{0, 0, 0, 0};
+    u32x4 af[MT][2], bf[4][2];  // [tile][step]
     const int at0 = c * kStage + ((q ^ (c & 7)) * 16);  // by rows: place of piece q of row c; of piece 4 + q: the same with bit 6 flipped
-    int at_a[4], at_b[2];
+    int at_a[MT], at_b[4 / B_REGIONS];
 #pragma unroll
-    for (int t = 0; t < 4; ++t) at_a[t] = A_ACROSS ? Across<T, 128>::address(wm * 4 + t, c, q) : wm * 64 * kStage + t * 16 * kStage + at0;
+    for (int t = 0; t < MT; ++t) at_a[t] = A_ACROSS ? Across<T, 128>::address(wm * MT + t, c, q) : (wm * MT + t) * 16 * kStage + at0;
+    // (two regions: two of the wave's tiles in each, at the same place)
+    constexpr int PLACES = 4 / B_REGIONS;
 #pragma unroll
-    for (int t = 0; t < 2; ++t) at_b[t] = B_ACROSS ? Across<T, 128>::address(wn * 2 + t, c, q) : wn * 32 * kStage + t * 16 * kStage + at0;
+    for (int t = 0; t < PLACES; ++t) {
+        const int tile = GATED && B_REGIONS == 1 ? (t >> 1) * (COLS / 16) + wn * 2 + (t & 1) : wn * PLACES + t;
+        at_b[t] = B_ACROSS ? Across<T, 128>::address(tile, c, q) : tile * 16 * kStage + at0;
+    }
     auto read_a = [&](int buf, int half) {
         const char* base = smem + buf * kBuffer + half * kRegion;
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
+        for (int t = 0; t < MT; ++t)
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
                 if constexpr (A_ACROSS) af[t][s] = Across<T, 128>::read(base + at_a[t] + s * (kRegion / 2));
@@ -148,11 +217,11 @@ __global__ __launch_bounds__(512, 2) void product_tiles_kernel(Product p, int ti
     auto read_b = [&](int buf) {
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
-            const char* base = smem + buf * kBuffer + (2 + (t >> 1)) * kRegion;
+            const char* base = smem + buf * kBuffer + (2 + t / PLACES) * kRegion;
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
-                if constexpr (B_ACROSS) bf[t][s] = Across<T, 128>::read(base + at_b[t & 1] + s * (kRegion / 2));
-                else bf[t][s] = *(const u32x4*)(base + (at_b[t & 1] ^ (s * 64)));
+                if constexpr (B_ACROSS) bf[t][s] = Across<T, 128>::read(base + at_b[t % PLACES] + s * (kRegion / 2));
+                else bf[t][s] = *(const u32x4*)(base + (at_b[t % PLACES] ^ (s * 64)));
             }
         }
     };
@@ -162,9 +231,9 @@ __global__ __launch_bounds__(512, 2) void product_tiles_kernel(Product p, int ti
 #pragma unroll
         for (int s = 0; s < 2; ++s)
 #pragma unroll
-            for (int t = 0; t < 4; ++t)
+            for (int t = 0; t < MT; ++t)
 #pragma unroll
-                for (int u = 0; u < 4; ++u) acc[ma * 4 + t][u] = Mma16<T>::mma(bf[u][s], af[t][s], acc[ma * 4 + t][u]);
+                for (int u = 0; u < 4; ++u) acc[ma * MT + t][u] = Mma16<T>::mma(bf[u][s], af[t][s], acc[ma * MT + t][u]);
         __builtin_amdgcn_s_setprio(0);
     };
     auto meet = [&] {
@@ -174,52 +243,75 @@ __global__ __launch_bounds__(512, 2) void product_tiles_kernel(Product p, int ti
         __builtin_amdgcn_sched_barrier(0);
         fence();
     };
-    auto landed = [&] {  // vmcnt(8): the copies of all but the four newest regions; lgkmcnt(0): operands
+    constexpr int BEHIND = 4 + 2 * B_REGIONS;
+    auto landed = [&] {  // vmcnt: the copies of all but the newest regions, two of A and those of B; lgkmcnt(0): operands
         fence();
-        __builtin_amdgcn_s_waitcnt(0x0070 | 8);
+        __builtin_amdgcn_s_waitcnt(ROWS == kWhole ? 0x0070 | BEHIND : 0xc07f);
     };
-    issue(0, 2), issue(0, 3), issue(0, 0), issue(0, 1), issue(1, 2), issue(1, 3), issue(1, 0);
+    auto issue_first = [&](int stage) {
+#pragma unroll
+        for (int r = 0; r < B_REGIONS; ++r) issue(stage, 2 + r);
+        issue(stage, 0);
+    };
+    if constexpr (ROWS == kWhole) {
+        issue_first(0), issue(0, 1), issue_first(1);
+    } else {
+        if (S > 0) {  // (a sum of nothing has no memory behind its operands)
+            load(0);
+            store(0);
+        }
+        if (S > 1) load(1);
+    }
     landed();
     meet();
-    if (wm) meet();  // the waves of one half are a part behind the others'
+    if (late) meet();  // half of the waves are a part behind the others
     for (int s = 0; s < S; ++s) {
         const bool part = rest < STAGE && (s == S - 1 || (FORM == kBackRows && s == S1 - 1));  // uniform: the sum ends in this stage
         read_b(s & 1);
         read_a(s & 1, 0);
-        issue(s + 1, 1);
+        if constexpr (ROWS == kWhole) issue(s + 1, 1);
         landed();
         meet();
-        if (part) {
+        if (ROWS == kWhole && part) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) clear_past(af[i >> 1][i & 1], i & 1), clear_past(bf[i >> 1][i & 1], i & 1);
+            for (int i = 0; i < 2 * MT; ++i) clear_past(af[i >> 1][i & 1], i & 1);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) clear_past(bf[i >> 1][i & 1], i & 1);
         }
         multiply(0);
         meet();
 
         read_a(s & 1, 1);
-        issue(s + 2, 2), issue(s + 2, 3), issue(s + 2, 0);
+        if constexpr (ROWS == kWhole) {
+            issue_first(s + 2);
+        } else if (s + 1 < S) {  // (the other buffer has been read: both groups of waves are past a barrier behind its last part)
+            store(s + 1);
+            if (s + 2 < S) load(s + 2);
+        }
         landed();
         meet();
-        if (part) {
+        if (ROWS == kWhole && part) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) clear_past(af[i >> 1][i & 1], i & 1);
+            for (int i = 0; i < 2 * MT; ++i) clear_past(af[i >> 1][i & 1], i & 1);
         }
         multiply(1);
         meet();
     }
-    if (!wm) meet();
+    if (!late) meet();
     __builtin_amdgcn_s_waitcnt(0x0f70);  // the surplus copies have landed: LDS may be given away
 
     // ---- results: a lane holds 16 neighbouring channels (gated: 8 of each projection; across: four times 4) of eight rows ----
     constexpr int RUN = GATED ? 8 : B_ACROSS ? 4 : 16, RUNS = B_ACROSS ? 4 : 1;
 #pragma unroll
     for (int u = 0; u < RUNS; ++u) {
-        const int n = n0 + (GATED ? wn * 32 : B_ACROSS ? (u >> 1) * 128 + wn * 32 + (u & 1) * 16 : wn * 64) + RUN * q;
+        // (across: 16 columns a tile, of 128 in a region)
+        const int column = B_REGIONS == 2 ? (u >> 1) * 128 + wn * 32 + (u & 1) * 16 : wn * 64 + u * 16;
+        const int n = n0 + (GATED ? wn * 32 : B_ACROSS ? column : wn * 64) + RUN * q;
         if (n >= p.N) continue;
         const RunOutput<FORM, T, TO, RUN> out(p, n);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int64_t m = m0 + (i >> 2) * 128 + wm * 64 + (i & 3) * 16 + c;
+        for (int i = 0; i < 2 * MT; ++i) {
+            const int64_t m = m0 + i / MT * 128 + (wm * MT + i % MT) * 16 + c;
             if (m >= p.M) continue;
             Acc first[RUN / 4], second[RUN / 4];
 #pragma unroll
@@ -232,18 +324,18 @@ __global__ __launch_bounds__(512, 2) void product_tiles_kernel(Product p, int ti
     }
 }
 
-template <typename T, typename TO, int FORM> rtoss_status launch(const Product& p, hipStream_t s)
+template <typename T, typename TO, int FORM, int TILE_N, int ROWS> rtoss_status launch(const Product& p, hipStream_t s)
 {
-    constexpr int COLS = FORM == kGated ? kTileN / 2 : kTileN;
+    constexpr int COLS = FORM == kGated ? TILE_N / 2 : TILE_N, LDS = 2 * (2 + TILE_N / 128) * kRegion;
     static LaunchOnce once;
     DeviceInfo dev;
     if (rtoss_status st = current_device(&dev)) return st;
-    const auto kernel = product_tiles_kernel<T, TO, FORM>;
-    if (rtoss_status st = ensure_dynamic_lds((const void*)kernel, 2 * kBuffer, once, dev.device, "LDS of a product")) return st;
+    const auto kernel = product_tiles_kernel<T, TO, FORM, TILE_N, ROWS>;
+    if (rtoss_status st = ensure_dynamic_lds((const void*)kernel, LDS, once, dev.device, "LDS of a product")) return st;
     const int tiles_m = (int)(((int64_t)p.M + kTileM - 1) / kTileM) * (FORM == kBackWeights ? 2 : 1), tiles_n = (p.N + COLS - 1) / COLS;
     const int64_t tiles = (int64_t)tiles_m * tiles_n;
     const int64_t per_xcd = (tiles + 7) / 8;
-    kernel<<<(unsigned)(per_xcd * 8), 512, 2 * kBuffer, s>>>(p, tiles_m, tiles_n, (int)tiles, (int)per_xcd);
+    kernel<<<(unsigned)(per_xcd * 8), 512, LDS, s>>>(p, tiles_m, tiles_n, (int)tiles, (int)per_xcd);
     return check_hip(hipGetLastError(), "product launch");
 }
 
@@ -261,30 +353,37 @@ bool product_pieces_ok(ProductForm form, const Product& p, int eb)
     return p.R > 0 && (b_across ? (int64_t)p.N * eb % 16 == 0 : (int64_t)p.R * eb % 16 == 0);
 }
 
-bool product_tiles_ok(ProductForm form, bool bits8, rtoss_dtype out, const Product& p)
+bool product_tiles_ok(bool bits8, rtoss_dtype out, const Product& p)
 {
-    if (!product_pieces_ok(form, p, bits8 ? 1 : elem_bytes(out))) return false;
-    const int cols = form == kGated ? kTileN / 2 : kTileN;
-    return (((int64_t)p.M + kTileM - 1) / kTileM) * ((p.N + cols - 1) / cols) <= kMaxGridGroups / 4;
+    return (bits8 || out != RTOSS_F32) && p.R > 0 && (((int64_t)p.M + kTileM - 1) / kTileM) * (((int64_t)p.N + 63) / 64) <= kMaxGridGroups / 4;
 }
 
 namespace {
-template <typename T> rtoss_status launch_form(ProductForm form, const Product& p, hipStream_t s)
+template <typename T, typename TO, int FORM> rtoss_status launch_width(bool wide, const Product& p, hipStream_t s)
 {
-    return form == kGated ? launch<T, T, kGated>(p, s) : form == kBackRows ? launch<T, T, kBackRows>(p, s) : launch<T, T, kBackWeights>(p, s);
+    switch (product_rows((ProductForm)FORM, p, (int)sizeof(T))) {
+    case kWhole: return wide ? launch<T, TO, FORM, 256, kWhole>(p, s) : launch<T, TO, FORM, 128, kWhole>(p, s);
+    case kWords: return launch<T, TO, FORM, 128, kWords>(p, s);
+    default: return launch<T, TO, FORM, 128, sizeof(T) == 4 ? kWords : kBytes>(p, s);  // (elements of four bytes are words)
+    }
 }
-template <typename TO> rtoss_status launch_bits8(ProductForm form, const Product& p, hipStream_t s)
+template <typename T> rtoss_status launch_form(ProductForm form, bool wide, const Product& p, hipStream_t s)
 {
-    return form == kScaled ? launch<int8_t, TO, kScaled>(p, s) : launch<int8_t, TO, kGated>(p, s);
+    return form == kGated ? launch_width<T, T, kGated>(wide, p, s) : form == kBackRows ? launch_width<T, T, kBackRows>(wide, p, s)
+                                                                                        : launch_width<T, T, kBackWeights>(wide, p, s);
+}
+template <typename TO> rtoss_status launch_bits8(ProductForm form, bool wide, const Product& p, hipStream_t s)
+{
+    return form == kScaled ? launch_width<int8_t, TO, kScaled>(wide, p, s) : launch_width<int8_t, TO, kGated>(wide, p, s);
 }
 }  // namespace
 
-rtoss_status launch_product_tiles(ProductForm form, bool bits8, rtoss_dtype out, const Product& p, hipStream_t s)
+rtoss_status launch_product_tiles(ProductForm form, bool bits8, rtoss_dtype out, bool wide, const Product& p, hipStream_t s)
 {
     switch (out) {
-    case RTOSS_F32: return bits8 ? launch_bits8<float>(form, p, s) : launch_form<float>(form, p, s);
-    case RTOSS_F16: return bits8 ? launch_bits8<f16_t>(form, p, s) : launch_form<f16_t>(form, p, s);
-    default: return bits8 ? launch_bits8<bf16_t>(form, p, s) : launch_form<bf16_t>(form, p, s);
+    case RTOSS_F32: return launch_bits8<float>(form, wide, p, s);  // (8-bit operands: product_tiles_ok)
+    case RTOSS_F16: return bits8 ? launch_bits8<f16_t>(form, wide, p, s) : launch_form<f16_t>(form, wide, p, s);
+    default: return bits8 ? launch_bits8<bf16_t>(form, wide, p, s) : launch_form<bf16_t>(form, wide, p, s);
     }
 }
 

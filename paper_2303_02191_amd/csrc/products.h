@@ -37,42 +37,6 @@ template <int N> __device__ __forceinline__ void gate_act(float (&v)[N], int act
     }
 }
 
-// Four neighbouring values of a row, `left` of which exist.  VEC: the row's runs of four are aligned to their size.
-template <typename TO> __device__ __forceinline__ void store4(TO* p, const float (&v)[4], int left, bool vec)
-{
-    if (vec && left >= 4) {
-        if constexpr (sizeof(TO) == 4) *(f32x4*)p = f32x4{v[0], v[1], v[2], v[3]};
-        else *(uint2*)p = uint2{pack2_from_f32<TO>(v[0], v[1]), pack2_from_f32<TO>(v[2], v[3])};
-        return;
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-        if (i < left) store_from_f32(p + i, v[i]);
-}
-template <typename TO> __device__ __forceinline__ void load4(const TO* p, float (&v)[4], int left, bool vec)
-{
-    if (vec && left >= 4) {
-        if constexpr (sizeof(TO) == 4) {
-            const f32x4 t = *(const f32x4*)p;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = t[i];
-        } else {
-            TO t[4];
-            *(uint2*)t = *(const uint2*)p;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = to_f32(t[i]);
-        }
-        return;
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = i < left ? to_f32(p[i]) : 0.f;
-}
-// Whether runs of four elements of TO that start at multiples of four in rows `ld` apart are aligned to their size.
-template <typename TO> __host__ __device__ __forceinline__ bool runs_of_4(const void* p, int64_t ld)
-{
-    return ((uintptr_t)p % (4 * sizeof(TO))) == 0 && ld % 4 == 0;
-}
-
 // Accumulators of the 16-bit types and fp32 are fp32, of 8-bit operands 32-bit integers (exact for R < 2^17).
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 template <typename T> struct AccOf { typedef f32x4 type; };
@@ -85,73 +49,19 @@ template <> struct Mma16<int8_t> {
     }
 };
 
-// Output stage for four neighbouring channels n .. n+3 of row m; `left` of them exist.  acc1: kGated's second sum.
-struct ProductVec {
-    bool y, kept, residual;  // runs of four are aligned
-};
-template <typename TO> __device__ __forceinline__ ProductVec product_vec(const Product& p)
-{
-    return ProductVec{runs_of_4<TO>(p.y, p.ldy), runs_of_4<TO>(p.y0, p.N) && runs_of_4<TO>(p.y1, p.N), runs_of_4<TO>(p.residual, p.ldr)};
-}
-template <typename T, typename ACC> __device__ __forceinline__ void scaled4(float (&v)[4], ACC acc, float sa, const float* s, int left)
-{
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        v[i] = (float)acc[i];  // (whole numbers above 2^24 round here, to 24 bits as every fp32 value)
-        if constexpr (sizeof(T) == 1) {
-            v[i] *= sa;
-            if (s && i < left) v[i] *= s[i];
-        }
-    }
-}
-template <int FORM, typename T, typename TO, typename ACC>
-__device__ __forceinline__ void product_output(const Product& p, const ProductVec& vec, int64_t m, int n, float sa, ACC acc0, ACC acc1)
-{
-    const int left = p.N - n;
-    if (left <= 0) return;
-    float v[4];
-    scaled4<T>(v, acc0, sa, p.s0 ? p.s0 + n : nullptr, left);
-    if constexpr (FORM == kScaled) {
-        if (p.bias)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] += i < left ? p.bias[n + i] : 0.f;
-        gate_act<4>(v, p.act);
-        if (p.residual) {
-            float r[4];
-            load4((const TO*)p.residual + m * p.ldr + n, r, left, vec.residual);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] += r[i];
-        }
-    } else if constexpr (FORM == kGated) {
-        float u[4];
-        scaled4<T>(u, acc1, sa, p.s1 ? p.s1 + n : nullptr, left);
-        if (p.y0) {
-            store4((TO*)p.y0 + m * p.N + n, v, left, vec.kept);
-            store4((TO*)p.y1 + m * p.N + n, u, left, vec.kept);
-        }
-        gate_act<4>(v, p.act);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] *= u[i];
-    }
-    store4((TO*)p.y + m * p.ldy + n, v, left, vec.y);
-}
-
 // ----- launchers -----
 rtoss_status launch_quantize_rows(const void* x, rtoss_dtype dt, int64_t M, int K, int64_t ldx, int8_t* q, int64_t ldq, float* scale,
                                   hipStream_t s);
-// kScaled and kGated on 8-bit operands, kGated and the gradients on operands of the result's type (product_any.hip)
-rtoss_status launch_product_any(ProductForm form, bool bits8, rtoss_dtype out, const Product& p, hipStream_t s);
-// kScaled and kGated of few rows, of any alignment (product_few.hip)
-bool product_few_ok(ProductForm form, const Product& p);
-rtoss_status launch_product_few(ProductForm form, bool bits8, rtoss_dtype out, const Product& p, hipStream_t s);
-// every form on whole 16-byte pieces of rows, in tiles of 256 x 256 results (product_tiles.hip)
-bool product_pieces_ok(ProductForm form, const Product& p, int eb);
-bool product_tiles_ok(ProductForm form, bool bits8, rtoss_dtype out, const Product& p);
-rtoss_status launch_product_tiles(ProductForm form, bool bits8, rtoss_dtype out, const Product& p, hipStream_t s);
-// the same in small tiles, 0: 64 x 64, 1: 128 x 64, 2: 128 x 128 (product_mid.hip)
-rtoss_status launch_product_mid(ProductForm form, bool bits8, rtoss_dtype out, int tile, const Product& p, hipStream_t s);
-// ... of few tiles: the sum split over the waves of a workgroup (product_slices.hip)
-rtoss_status launch_product_slices(ProductForm form, bool bits8, rtoss_dtype out, const Product& p, hipStream_t s);
+// Every form: kScaled and kGated on 8-bit operands, kGated and the gradients on operands of the result's type.
+bool product_pieces_ok(ProductForm form, const Product& p, int eb);  // rows are whole 16-byte pieces (product_tiles.hip)
+// ... in tiles of 256 rows and 256 (wide) or 128 channels, of 8- and 16-bit operands (product_tiles.hip)
+bool product_tiles_ok(bool bits8, rtoss_dtype out, const Product& p);
+rtoss_status launch_product_tiles(ProductForm form, bool bits8, rtoss_dtype out, bool wide, const Product& p, hipStream_t s);
+// ... of few tiles, and fp32: the sum split over the waves of a workgroup (product_slices.hip).  The tile, rows x channels of a matrix: kSlices;
+// gradients take the last.
+constexpr int kSliceTiles = 5;
+constexpr struct { int rows, channels, gated; } kSlices[kSliceTiles] = {{16, 16, 16}, {32, 16, 16}, {32, 32, 32}, {64, 32, 16}, {64, 64, 32}};
+rtoss_status launch_product_slices(ProductForm form, bool bits8, rtoss_dtype out, int tile, const Product& p, hipStream_t s);
 // dg = dh * u * act'(g), du = dh * act(g), both [M][ldd] with zeros from column F on (gated_slopes.hip); ldd: slopes_pitch
 inline int64_t slopes_pitch(int F, rtoss_dtype dt) { return (int64_t)align_up((size_t)F, 16 / elem_bytes(dt)); }
 rtoss_status launch_gated_slopes(rtoss_dtype dt, rtoss_act act, int64_t M, int F, const void* dh, int64_t ldh, const void* gate, const void* up,

@@ -1,7 +1,7 @@
 // C entries of the 8-bit products and the gated feed-forward block: checks of the arguments (before any HIP call) and the choice of
 // kernels.
 #include <algorithm>
-#include <cstdlib>
+#include <cmath>
 
 #include "products.h"
 
@@ -74,18 +74,43 @@ rtoss_status gated_desc(const rtoss_gated_desc* desc, rtoss_gated_desc* d)
     return RTOSS_OK;
 }
 
+// The kernel for a product: the one whose estimate is shortest.  All are bound by what a CU can copy in the small, by the matrix instructions
+// in the large, and by whole rounds of workgroups.  Constants as measured (us, 256 CUs; M x K x N):
+//   slices of a x b: the launch 3.4 (64 x 64: 4.6), then 80 KB/us and CU for the rows of both operands.  8-bit 4096 x 4096, rows 1, 64, 128, 256, 512:
+//     5.1, 6.8, 7.8, 10.2, 17.6 with the tile that this takes; 8.5, 9.6, 9.6, 10.2, 17.6 with 64 x 64 for all.
+//   tiles: 6 and 8, then 0.95 and 1.3 a stage of 128 bytes (128 and 256 channels).  Gated bf16 4096 -> 10944, rows 256, 512, 1000, 2048: 62, 117,
+//     183, 360 with 128, 83, 90, 173, 284 with 256 channels; slices of 64 x 64 104, 178, 352, 850.
 rtoss_status launch_product(ProductForm form, bool bits8, rtoss_dtype out, const Product& p, hipStream_t s)
 {
-    const char* force = getenv("RTOSS_FORCE");
-    const int f = force ? atoi(force) : -1;
-    if (f == 7) return launch_product_slices(form, bits8, out, p, s);
-    if (f == 9 || !product_tiles_ok(form, bits8, out, p)) { if (product_few_ok(form, p) && f != 9) return launch_product_few(form, bits8, out, p, s); return launch_product_any(form, bits8, out, p, s); }
-    if ((f >= 0 && f < 3) || (f >= 4 && f < 7)) return launch_product_mid(form, bits8, out, f, p, s);
-    if (f == 7) return launch_product_slices(form, bits8, out, p, s);
-    if (f == 3) return launch_product_tiles(form, bits8, out, p, s);
-    if (product_few_ok(form, p)) return launch_product_few(form, bits8, out, p, s);
-    if (p.M > 128) return launch_product_tiles(form, bits8, out, p, s);
-    return launch_product_any(form, bits8, out, p, s);
+    DeviceInfo dev;
+    RTOSS_TRY(current_device(&dev));
+    const int eb = bits8 ? 1 : elem_bytes(out);
+    const bool gated = form == kGated, across = form == kBackRows || form == kBackWeights;
+    const double row = (double)p.R * eb * (form == kBackRows ? 2 : 1), cus = dev.cus;
+    const auto up = [](int64_t n, int by) { return (double)((n + by - 1) / by); };
+    const auto tiles = [&](int rows, int channels) { return up(p.M, rows) * up(p.N, channels) * (form == kBackWeights ? 2 : 1); };
+    int best = kSliceTiles - 1;  // slices by tile, then the two widths
+    double least = 1e300;
+    for (int t = across ? kSliceTiles - 1 : 0; t < kSliceTiles; ++t) {
+        const int a = kSlices[t].rows, n = gated ? kSlices[t].gated : kSlices[t].channels, b = gated ? 2 * n : n;
+        const double count = tiles(a, n) / cus;
+        const int together = 160 / (a + b);  // workgroups whose LDS a CU holds
+        const double rounds = together >= 2 ? std::max(1.0, count) : std::ceil(count);
+        const double one = std::max((a + b) * row / 80e3, eb == 4 ? a * b * row / eb / 500e3 : 0.0);
+        const double time = (a + b >= 128 ? 4.6 : a + b >= 96 ? 3.8 : 3.4) + rounds * one;
+        if (time < least) least = time, best = t;
+    }
+    if (product_tiles_ok(bits8, out, p)) {
+        const double stages = std::ceil(row / 128);
+        const bool whole = product_pieces_ok(form, p, eb);
+        for (int wide = 0; wide <= (whole ? 1 : 0); ++wide) {
+            const int n = (wide ? 256 : 128) / (gated ? 2 : 1);
+            const double time = (wide ? 8 : 6) + std::ceil(tiles(256, n) / cus) * stages * (wide ? 1.3 : 0.95);
+            if (time < least) least = time, best = kSliceTiles + wide;
+        }
+    }
+    if (best < kSliceTiles) return launch_product_slices(form, bits8, out, best, p, s);
+    return launch_product_tiles(form, bits8, out, best > kSliceTiles, p, s);
 }
 
 size_t slopes_bytes(const rtoss_gated_desc& d) { return align_up((size_t)d.M * slopes_pitch(d.F, d.dt) * elem_bytes(d.dt), 256); }
