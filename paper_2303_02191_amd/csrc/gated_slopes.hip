@@ -28,23 +28,26 @@ template <typename T, int ACT> __device__ __forceinline__ void slopes(float g, f
     }
 }
 
-// A lane takes 16 bytes of dg and du at a time, row by row; ldd is a whole number of such pieces, with zeros past the row's end.  VEC: so
-// are the rows of the inputs.
+// A lane takes 16 bytes of dg and du at a time; their rows are whole numbers of such pieces, with zeros past the row's end.  VEC: so are the
+// rows of the inputs, without gaps.
 template <typename T, int ACT, bool VEC>
 __global__ __launch_bounds__(256) void gated_slopes_kernel(const T* __restrict__ dh, const T* __restrict__ gate, const T* __restrict__ up,
                                                            T* __restrict__ dg, T* __restrict__ du, int64_t pieces, int per_row, int F, int64_t ldh)
 {
     constexpr int E = 16 / (int)sizeof(T);
-    const int64_t step = (int64_t)gridDim.x * 256;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < pieces; i += step) {
+    // VEC: one run of pieces; otherwise a row of workgroups for each row (or every gridDim.y-th), so that there is none to find
+    const int64_t step = VEC ? (int64_t)gridDim.x * 256 : per_row * (int64_t)gridDim.y;
+    const int at = (int)blockIdx.x * 256 + (int)threadIdx.x;
+    if (!VEC && at >= per_row) return;
+    int64_t m = blockIdx.y;
+    for (int64_t i = VEC ? at : m * per_row + at; i < pieces; i += step, m += gridDim.y) {
         T g[E], u[E], h[E], og[E], ou[E];
-        if (VEC && ldh == F) {  // one run: no rows to find
+        if (VEC) {
             *(u32x4*)g = *(const u32x4*)(gate + i * E);
             *(u32x4*)u = *(const u32x4*)(up + i * E);
             *(u32x4*)h = *(const u32x4*)(dh + i * E);
         } else {
-            const int64_t m = i / per_row;
-            const int f = (int)(i - m * per_row) * E;
+            const int f = at * E;
             const T *pg = gate + m * F + f, *pu = up + m * F + f, *ph = dh + m * ldh + f;
             if (f + E <= F) {  // (at whatever address)
                 __builtin_memcpy(g, pg, 16);
@@ -74,10 +77,10 @@ template <typename T>
 rtoss_status launch(rtoss_act act, int64_t M, int F, const void* dh, int64_t ldh, const void* gate, const void* up, void* dg, void* du, hipStream_t s)
 {
     constexpr int E = 16 / (int)sizeof(T);
-    const bool vec = F % E == 0 && ((uintptr_t)dh | (uintptr_t)gate | (uintptr_t)up) % 16 == 0;
+    const bool vec = F % E == 0 && ldh == F && ((uintptr_t)dh | (uintptr_t)gate | (uintptr_t)up) % 16 == 0;
     const int per_row = (F + E - 1) / E;
     const int64_t pieces = M * per_row;
-    const unsigned grid = (unsigned)std::min<int64_t>((pieces + 255) / 256, 16384);
+    const dim3 grid = vec ? dim3((unsigned)std::min<int64_t>((pieces + 255) / 256, 16384)) : dim3((per_row + 255) / 256, (unsigned)std::min<int64_t>(M, 16384));
     auto go = [&](auto kernel) {
         kernel<<<grid, 256, 0, s>>>((const T*)dh, (const T*)gate, (const T*)up, (T*)dg, (T*)du, pieces, per_row, F, ldh);
         return check_hip(hipGetLastError(), "gated_slopes launch");

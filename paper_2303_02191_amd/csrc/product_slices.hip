@@ -15,10 +15,9 @@ namespace rtoss {
 
 namespace {
 
-constexpr int kWaves = 8;
-
-template <typename T, typename TO, int FORM, int ROWS, int BM, int BN>
-__global__ __launch_bounds__(64 * kWaves, 2) void product_slices_kernel(Product p, int tiles_m, int tiles_n, int tiles, int per_xcd)
+// One tile of a product, `work` of tiles_m x tiles_n.
+template <typename T, typename TO, int FORM, int ROWS, int BM, int BN, int WAVES>
+__device__ __forceinline__ void product_slices(Product p, int work, int tiles_m, int tiles_n)
 {
     typedef typename AccOf<T>::type Acc;
     constexpr bool GATED = FORM == kGated;
@@ -33,9 +32,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void product_slices_kernel(Product 
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c = lane & 15, q = lane >> 4;
 
-    // XCD-contiguous, in groups of eight row tiles, rows fastest: the workgroups that run on an XCD at a time share rows and channels in its L2
-    const int work = (int)(blockIdx.x % 8) * per_xcd + (int)(blockIdx.x / 8);
-    if (work >= tiles) return;
+    // in groups of eight row tiles, rows fastest: the workgroups that run on an XCD at a time share rows and channels in its L2
     constexpr int GROUP = 8;
     const int group = work / (GROUP * tiles_n), in_group = work - group * (GROUP * tiles_n);
     const int high = min(GROUP, tiles_m - group * GROUP);
@@ -52,7 +49,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void product_slices_kernel(Product 
     const int64_t m0 = (int64_t)tile_m * BM;
 
     const int64_t lda = p.lda * EB, ldb = p.ldb * EB, row = (int64_t)p.R * EB;
-    const int S1 = (p.R + STAGE - 1) / STAGE, S = FORM == kBackRows ? 2 * S1 : S1;
+    const int S1 = (int)(((int64_t)p.R + STAGE - 1) / STAGE), S = FORM == kBackRows ? 2 * S1 : S1;
     const int rest = p.R - (S1 - 1) * STAGE;  // rows of the sum in the last stage
     auto whole = [](int64_t bytes) { return (bytes + 15) & ~(int64_t)15; };  // (dg and du, whose rows are padded)
     auto rows_from = [&](const void* base, int64_t ld, int64_t first, int64_t rows) {
@@ -126,25 +123,25 @@ __global__ __launch_bounds__(64 * kWaves, 2) void product_slices_kernel(Product 
     for (int t = 0; t < MT; ++t) at_a[t] = A_ACROSS ? AcrossA::address(t, c, q) : t * 16 * kStage + at0;
 #pragma unroll
     for (int t = 0; t < NT; ++t) at_b[t] = A_BYTES + (B_ACROSS ? AcrossB::address(t, c, q) : t * 16 * kStage + at0);
-    // ---- what the output stage reads, before the sum.  Wave w stores unit w: of a row tile, PART channel tiles (gated: one of each projection)
+    // ---- what the output stage reads, before the sum.  Wave w stores the units w, w + WAVES, ..: of a row tile, PART channel tiles (gated: one of
+    // each projection); it reads ahead for the first
     constexpr int PART = NT == 1 ? 1 : 2, SHARE = NT / PART, UNITS = MT * SHARE;
-    static_assert(UNITS <= kWaves && (!GATED || NT >= 2), "a wave's share of the results");
-    const int row_tile = wave / SHARE % MT, share = wave % SHARE;
-    const int64_t m = m0 + row_tile * 16 + c;
+    static_assert(!GATED || NT >= 2, "a wave's share of the results");
     // a lane's channels: 4 PART neighbouring ones; gated: 4 of each projection; across: 4 of each tile
     constexpr int RUN = GATED || B_ACROSS ? 4 : 4 * PART, RUNS = B_ACROSS ? PART : 1;
-    int n_out[RUNS];
-#pragma unroll
-    for (int u = 0; u < RUNS; ++u)
-        n_out[u] = n0 + (B_ACROSS ? (PART * share + u) * 16 + 4 * q : GATED ? 2 * NT * q + 4 * share : 4 * NT * q + 4 * PART * share);
+    auto row_of = [&](int unit) { return m0 + unit / SHARE * 16 + c; };
+    auto channel_of = [&](int unit, int u) {
+        const int share = unit % SHARE;
+        return n0 + (B_ACROSS ? (PART * share + u) * 16 + 4 * q : GATED ? 2 * NT * q + 4 * share : 4 * NT * q + 4 * PART * share);
+    };
     typedef RunOutput<FORM, T, TO, RUN> Output;
-    const Output out(p, min(n_out[0], p.N - 1));  // (across: it holds nothing but the place)
-    const float sa = Output::kScales && p.sa ? p.sa[min(m, (int64_t)p.M - 1)] : 1.f;
+    auto scale_of = [&](int64_t m) { return Output::kScales && p.sa ? p.sa[min(m, (int64_t)p.M - 1)] : 1.f; };
+    const Output first_out(p, min(channel_of(wave, 0), p.N - 1));  // (across: it holds nothing but the place)
+    const float first_scale = scale_of(row_of(wave));
 
     auto read_and_multiply = [&](const char* base, int s, auto&& then) {
         u32x4 af[2][MT], bf[2][NT];
-#pragma unroll
-        for (int step = 0; step < 2; ++step) {
+        auto read_step = [&](int step) {
 #pragma unroll
             for (int t = 0; t < MT; ++t) {
                 if constexpr (A_ACROSS) af[step][t] = AcrossA::read(base + at_a[t] + step * (A_BYTES / 2));
@@ -155,7 +152,24 @@ __global__ __launch_bounds__(64 * kWaves, 2) void product_slices_kernel(Product 
                 if constexpr (B_ACROSS) bf[step][t] = AcrossB::read(base + at_b[t] + step * (B_BYTES / 2));
                 else bf[step][t] = *(const u32x4*)(base + (at_b[t] ^ (step * 64)));
             }
+        };
+        auto multiply_step = [&](int step) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int i = 0; i < MT; ++i) acc[i][n] = Mma16<T>::mma(bf[step][n], af[step][i], acc[i][n]);
+        };
+        if constexpr (ROWS != kWhole && EB < 4) {  // (the next stage is in registers too: one step at a time)
+#pragma unroll
+            for (int step = 0; step < 2; ++step) {
+                read_step(step);
+                multiply_step(step);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            return;
         }
+        read_step(0);
+        read_step(1);
         then();
         if (ROWS == kWhole && __builtin_expect(rest < STAGE && (s == S - 1 || (FORM == kBackRows && s == S1 - 1)), 0)) {  // uniform: the sum ends here
 #pragma unroll
@@ -181,12 +195,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void product_slices_kernel(Product 
                 });
             }
         } else {
-#pragma unroll
-            for (int step = 0; step < 2; ++step)
-#pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int i = 0; i < MT; ++i) acc[i][n] = Mma16<T>::mma(bf[step][n], af[step][i], acc[i][n]);
+            multiply_step(0);
+            multiply_step(1);
         }
     };
     if constexpr (ROWS == kWhole) {
@@ -195,7 +205,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void product_slices_kernel(Product 
             static_for<PIECES>([&](auto k) { copy(f, lds0, k); });
         };
         if (wave < S) issue(wave);
-        for (int s = wave; s < S; s += kWaves) {
+        for (int s = wave; s < S; s += WAVES) {
             fence();
             __builtin_amdgcn_s_waitcnt(0x0f70);  // the stage has landed
             fence();
@@ -203,7 +213,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void product_slices_kernel(Product 
                 fence();
                 __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): its place is free
                 fence();
-                if (s + kWaves < S) issue(s + kWaves);
+                if (s + WAVES < S) issue(s + WAVES);
                 __builtin_amdgcn_sched_barrier(0);
             });
         }
@@ -237,18 +247,43 @@ __global__ __launch_bounds__(64 * kWaves, 2) void product_slices_kernel(Product 
             const int n = min(n0 + 4 * TILES * (r >> 2) + 4 * t + (r & 3), p.N - 1);
             return (const char*)(GATED && rho >= COLS ? p.b1 : p.b0) + n * ld + (int64_t)r_at * EB;
         };
-        // whether every piece of the stage is whole: uniform
-        auto inside = [&](int st) {
+        // Where all pieces of a stage can be loaded whole: a piece's offset from the tile does not change, its stage moves a uniform base.  (Rows
+        // past the last are the last again.  Across, columns past the last are what lies behind, in the row after: not the last one's.)
+        uint32_t at_piece[PIECES];
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            const bool of_a = i < A_COPIES;
+            const int k = of_a ? i : i - A_COPIES;
+            const uint32_t ld = (uint32_t)(of_a ? lda : ldb);
+            if (of_a ? A_ACROSS : B_ACROSS) {
+                const int r = k * AcrossA::kCopyRows + lane / AcrossA::kPieces, at = (lane % AcrossA::kPieces ^ AcrossA::spread(r)) * E;
+                const int last = (int)min(of_a ? p.M - m0 : (int64_t)(p.N - n0), (int64_t)64) - 1;
+                at_piece[i] = r * ld + (uint32_t)(min(at, last / E * E) * EB);
+            } else {
+                const int rho = k * 8 + sub, in = rho % COLS;
+                constexpr int TILES = GATED ? NT / 2 : NT;
+                const int row_at = of_a ? (int)min((int64_t)rho, p.M - 1 - m0) : min(4 * TILES * ((in & 15) >> 2) + 4 * (in / 16) + (in & 3), p.N - 1 - n0);
+                at_piece[i] = row_at * ld + piece * 16;
+            }
+        }
+        auto place_whole = [&](int i, int st) {
+            const bool second = FORM == kBackRows && st >= S1, of_a = i < A_COPIES;
+            if (second) st -= S1;
+            const void* base = of_a ? (second ? p.a1 : p.a0) : second || (GATED && i - A_COPIES >= B_COPIES / 2) ? p.b1 : p.b0;
+            const bool across = of_a ? A_ACROSS : B_ACROSS;
+            const int64_t ld = of_a ? lda : ldb, first = of_a ? m0 : (int64_t)n0;
+            return (const char*)base + (across ? first * EB + (int64_t)st * STAGE * ld : first * ld + (int64_t)st * kStage) + at_piece[i];
+        };
+        const bool near = lda <= 1 << 24 && ldb <= 1 << 24;  // (of further rows every piece is found by itself)
+        auto inside = [&](int st) {  // uniform
             if (FORM == kBackRows && st >= S1) st -= S1;
-            return (st + 1) * (int64_t)STAGE <= p.R && (!A_ACROSS || m0 + BM <= p.M) && (!B_ACROSS || n0 + BN <= p.N);
+            const int64_t end = (st + 1) * (int64_t)STAGE;
+            return near && (A_ACROSS || B_ACROSS ? end < p.R && (!A_ACROSS || lda >= 16) && ldb >= 16 : end <= p.R);
         };
         auto load = [&](int st) {
             if (inside(st)) {
 #pragma unroll
-                for (int i = 0; i < PIECES; ++i) {
-                    int have;
-                    piece_in[i].load(place(i, st, have));
-                }
+                for (int i = 0; i < PIECES; ++i) piece_in[i].load(place_whole(i, st));
             } else {
 #pragma unroll
                 for (int i = 0; i < PIECES; ++i) {
@@ -260,20 +295,25 @@ __global__ __launch_bounds__(64 * kWaves, 2) void product_slices_kernel(Product 
             }
         };
         auto store = [&](int st) {
-            const bool whole_stage = inside(st);
+            auto to = [&](int i) { return (u32x4*)(own + (i < A_COPIES ? i * 1024 : A_BYTES + (i - A_COPIES) * 1024) + lane * 16); };
+            if (inside(st)) {
 #pragma unroll
-            for (int i = 0; i < PIECES; ++i) {
-                int have;
-                const char* at = place(i, st, have);
-                u32x4 v = piece_in[i].value((uint32_t)(uintptr_t)at);  // (words that do not exist: other ones, cut off here)
-                if (!whole_stage) keep_first<T>(v, have);
-                *(u32x4*)(own + (i < A_COPIES ? i * 1024 : A_BYTES + (i - A_COPIES) * 1024) + lane * 16) = v;
+                for (int i = 0; i < PIECES; ++i) *to(i) = piece_in[i].value((uint32_t)(uintptr_t)place_whole(i, st));
+            } else {
+#pragma unroll
+                for (int i = 0; i < PIECES; ++i) {
+                    int have;
+                    const char* at = place(i, st, have);
+                    u32x4 v = piece_in[i].value((uint32_t)(uintptr_t)at);  // (words that do not exist: other ones, cut off here)
+                    keep_first<T>(v, have);
+                    *to(i) = v;
+                }
             }
         };
         if (wave < S) load(wave);
-        for (int s = wave; s < S; s += kWaves) {
+        for (int s = wave; s < S; s += WAVES) {
             store(s);
-            if (s + kWaves < S) load(s + kWaves);
+            if (s + WAVES < S) load(s + WAVES);
             fence();
             read_and_multiply(own, s, [&] {});
             fence();
@@ -289,42 +329,87 @@ __global__ __launch_bounds__(64 * kWaves, 2) void product_slices_kernel(Product 
 #pragma unroll
         for (int n = 0; n < NT; ++n) joined[((wave * MT + i) * NT + n) * 64 + lane] = acc[i][n];
     __syncthreads();
-    if (wave >= UNITS) return;
-    Acc sum[PART];
+    auto finish = [&](int unit, const Output& out, float sa) {
+        const int64_t m = row_of(unit);
+        const int share = unit % SHARE;
+        Acc sum[PART];
 #pragma unroll
-    for (int t = 0; t < PART; ++t) {
-        const Acc* from = joined + (row_tile * NT + (GATED ? NT / 2 * t + share : PART * share + t)) * 64 + lane;
-        sum[t] = from[0];
+        for (int t = 0; t < PART; ++t) {
+            const Acc* from = joined + (unit / SHARE * NT + (GATED ? NT / 2 * t + share : PART * share + t)) * 64 + lane;
+            sum[t] = from[0];
 #pragma unroll
-        for (int w = 1; w < kWaves; ++w) sum[t] += from[w * MT * NT * 64];
-    }
-    if (m >= p.M) return;
-#pragma unroll
-    for (int u = 0; u < RUNS; ++u) {
-        if (n_out[u] >= p.N) continue;
-        if constexpr (B_ACROSS) {
-            const Acc one[1] = {sum[u]};
-            Output(p, n_out[u]).store(p, m, sa, one, one);
-        } else if constexpr (GATED) {
-            const Acc first[1] = {sum[0]}, second[1] = {sum[PART - 1]};
-            out.store(p, m, sa, first, second);
-        } else {
-            out.store(p, m, sa, sum, sum);
+            for (int w = 1; w < WAVES; ++w) sum[t] += from[w * MT * NT * 64];
         }
+        if (m >= p.M) return;
+#pragma unroll
+        for (int u = 0; u < RUNS; ++u) {
+            const int n = channel_of(unit, u);
+            if (n >= p.N) continue;
+            if constexpr (B_ACROSS) {
+                const Acc one[1] = {sum[u]};
+                Output(p, n).store(p, m, sa, one, one);
+            } else if constexpr (GATED) {
+                const Acc first[1] = {sum[0]}, second[1] = {sum[PART - 1]};
+                out.store(p, m, sa, first, second);
+            } else {
+                out.store(p, m, sa, sum, sum);
+            }
+        }
+    };
+    if (wave < UNITS) finish(wave, first_out, first_scale);
+    for (int unit = wave + WAVES; unit < UNITS; unit += WAVES) finish(unit, Output(p, min(channel_of(unit, 0), p.N - 1)), scale_of(row_of(unit)));
+}
+
+template <typename T, typename TO, int FORM, int ROWS, int BM, int BN, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 2) void product_slices_kernel(Product p, int tiles_m, int tiles_n, int tiles, int per_xcd)
+{
+    const int work = (int)(blockIdx.x % 8) * per_xcd + (int)(blockIdx.x / 8);  // (XCD-contiguous)
+    if (work < tiles) product_slices<T, TO, FORM, ROWS, BM, BN, WAVES>(p, work, tiles_m, tiles_n);
+}
+
+// Both gradients in one launch (or one, by the same code): they share nothing but dg and du, and each alone leaves most of the chip without work.
+template <typename T, int ROWS, int BM, int WAVES>
+// Every XCD has its share of the rows' tiles, whose sums are long, and behind them its share of the weights'.
+__global__ __launch_bounds__(64 * WAVES, 2) void product_slices_back_kernel(Product rows, Product weights, int rows_m, int rows_n, int rows_per_xcd,
+                                                                            int weights_m, int weights_n, int weights_per_xcd)
+{
+    const int xcd = (int)(blockIdx.x % 8), at = (int)(blockIdx.x / 8);
+    if (at < rows_per_xcd) {
+        const int work = xcd * rows_per_xcd + at;
+        if (work < rows_m * rows_n) product_slices<T, T, kBackRows, ROWS, BM, 64, WAVES>(rows, work, rows_m, rows_n);
+    } else {
+        const int work = xcd * weights_per_xcd + at - rows_per_xcd;
+        if (work < weights_m * weights_n) product_slices<T, T, kBackWeights, ROWS, 64, 64, WAVES>(weights, work, weights_m, weights_n);
     }
 }
 
 template <typename T, typename TO, int FORM, int ROWS, int BM, int BN> rtoss_status launch(const Product& p, hipStream_t s)
 {
-    constexpr int COLS = FORM == kGated ? BN / 2 : BN, LDS = kWaves * (BM + BN) * kStage;
+    constexpr int WAVES = 8, COLS = FORM == kGated ? BN / 2 : BN, LDS = WAVES * (BM + BN) * kStage;
     static LaunchOnce once;
     DeviceInfo dev;
     if (rtoss_status st = current_device(&dev)) return st;
-    const auto kernel = product_slices_kernel<T, TO, FORM, ROWS, BM, BN>;
+    const auto kernel = product_slices_kernel<T, TO, FORM, ROWS, BM, BN, WAVES>;
     if (rtoss_status st = ensure_dynamic_lds((const void*)kernel, LDS, once, dev.device, "LDS of a product")) return st;
     const int tiles_m = (int)(((int64_t)p.M + BM - 1) / BM) * (FORM == kBackWeights ? 2 : 1), tiles_n = (p.N + COLS - 1) / COLS;
     const int64_t tiles = (int64_t)tiles_m * tiles_n, per_xcd = (tiles + 7) / 8;
-    kernel<<<(unsigned)(per_xcd * 8), 64 * kWaves, LDS, s>>>(p, tiles_m, tiles_n, (int)tiles, (int)per_xcd);
+    kernel<<<(unsigned)(per_xcd * 8), 64 * WAVES, LDS, s>>>(p, tiles_m, tiles_n, (int)tiles, (int)per_xcd);
+    return check_hip(hipGetLastError(), "product launch");
+}
+
+template <typename T, int ROWS, int BM> rtoss_status launch_back(const Product& rows, const Product& weights, hipStream_t s)
+{
+    constexpr int WAVES = 4, LDS = WAVES * (64 + 64) * kStage;
+    static LaunchOnce once;
+    DeviceInfo dev;
+    if (rtoss_status st = current_device(&dev)) return st;
+    const auto kernel = product_slices_back_kernel<T, ROWS, BM, WAVES>;
+    if (rtoss_status st = ensure_dynamic_lds((const void*)kernel, LDS, once, dev.device, "LDS of a product")) return st;
+    const auto up = [](int64_t n, int by) { return (int)((n + by - 1) / by); };  // (of no result: none)
+    const int rows_m = rows.y ? up(rows.M, BM) : 0, rows_n = up(rows.N, 64), weights_m = weights.y ? 2 * up(weights.M, 64) : 0, weights_n = up(weights.N, 64);
+    const int64_t rows_per_xcd = ((int64_t)rows_m * rows_n + 7) / 8, weights_per_xcd = ((int64_t)weights_m * weights_n + 7) / 8;
+    kernel<<<(unsigned)((rows_per_xcd + weights_per_xcd) * 8), 64 * WAVES, LDS, s>>>(rows, weights, rows_m, rows_n, (int)rows_per_xcd, weights_m, weights_n,
+                                                                                       (int)weights_per_xcd);
     return check_hip(hipGetLastError(), "product launch");
 }
 
@@ -369,6 +454,30 @@ rtoss_status launch_product_slices(ProductForm form, bool bits8, rtoss_dtype out
     case RTOSS_F32: return bits8 ? launch_bits8<float>(form, tile, p, s) : launch_form<float>(form, tile, p, s);
     case RTOSS_F16: return bits8 ? launch_bits8<f16_t>(form, tile, p, s) : launch_form<f16_t>(form, tile, p, s);
     default: return bits8 ? launch_bits8<bf16_t>(form, tile, p, s) : launch_form<bf16_t>(form, tile, p, s);
+    }
+}
+
+namespace {
+template <typename T> rtoss_status launch_back_rows(bool high, const Product& rows, const Product& weights, hipStream_t s)
+{
+    const auto tile = [&](auto mode) {
+        constexpr int ROWS = decltype(mode)::value;
+        return high ? launch_back<T, ROWS, 64>(rows, weights, s) : launch_back<T, ROWS, 16>(rows, weights, s);
+    };
+    switch (std::max(product_rows(kBackRows, rows, (int)sizeof(T)), product_rows(kBackWeights, weights, (int)sizeof(T)))) {
+    case kWhole: return tile(std::integral_constant<int, kWhole>{});
+    case kWords: return tile(std::integral_constant<int, kWords>{});
+    default: return tile(std::integral_constant<int, sizeof(T) == 4 ? kWords : kBytes>{});
+    }
+}
+}  // namespace
+
+rtoss_status launch_product_slices_back(rtoss_dtype dt, bool high, const Product& rows, const Product& weights, hipStream_t s)
+{
+    switch (dt) {
+    case RTOSS_F32: return launch_back_rows<float>(high, rows, weights, s);
+    case RTOSS_F16: return launch_back_rows<f16_t>(high, rows, weights, s);
+    default: return launch_back_rows<bf16_t>(high, rows, weights, s);
     }
 }
 

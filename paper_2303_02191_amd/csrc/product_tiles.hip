@@ -71,7 +71,7 @@ __global__ __launch_bounds__(512, 2) void product_tiles_kernel(Product p, int ti
     const int n0 = at / high * COLS;
 
     const int64_t lda = p.lda * EB, ldb = p.ldb * EB, row = (int64_t)p.R * EB;
-    const int S1 = (p.R + STAGE - 1) / STAGE, S = FORM == kBackRows ? 2 * S1 : S1;
+    const int S1 = (int)(((int64_t)p.R + STAGE - 1) / STAGE), S = FORM == kBackRows ? 2 * S1 : S1;
     const int rest = p.R - (S1 - 1) * STAGE;  // rows of the sum in the last stage
     auto whole = [](int64_t bytes) { return (bytes + 15) & ~(int64_t)15; };  // (dg and du, whose rows are padded)
     auto rows_from = [&](const void* base, int64_t ld, int64_t first, int64_t rows) {

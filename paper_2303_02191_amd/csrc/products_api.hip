@@ -80,37 +80,98 @@ rtoss_status gated_desc(const rtoss_gated_desc* desc, rtoss_gated_desc* d)
 //     5.1, 6.8, 7.8, 10.2, 17.6 with the tile that this takes; 8.5, 9.6, 9.6, 10.2, 17.6 with 64 x 64 for all.
 //   tiles: 6 and 8, then 0.95 and 1.3 a stage of 128 bytes (128 and 256 channels).  Gated bf16 4096 -> 10944, rows 256, 512, 1000, 2048: 62, 117,
 //     183, 360 with 128, 83, 90, 173, 284 with 256 channels; slices of 64 x 64 104, 178, 352, 850.
-rtoss_status launch_product(ProductForm form, bool bits8, rtoss_dtype out, const Product& p, hipStream_t s)
+struct Choice {
+    int kernel;   // slices by tile, then the two widths of tiles
+    double time;  // us
+};
+Choice choose(ProductForm form, bool bits8, rtoss_dtype out, const Product& p, int cus)
 {
-    DeviceInfo dev;
-    RTOSS_TRY(current_device(&dev));
     const int eb = bits8 ? 1 : elem_bytes(out);
     const bool gated = form == kGated, across = form == kBackRows || form == kBackWeights;
-    const double row = (double)p.R * eb * (form == kBackRows ? 2 : 1), cus = dev.cus;
+    const double row = (double)p.R * eb * (form == kBackRows ? 2 : 1);
     const auto up = [](int64_t n, int by) { return (double)((n + by - 1) / by); };
     const auto tiles = [&](int rows, int channels) { return up(p.M, rows) * up(p.N, channels) * (form == kBackWeights ? 2 : 1); };
-    int best = kSliceTiles - 1;  // slices by tile, then the two widths
-    double least = 1e300;
+    Choice best{kSliceTiles - 1, 1e300};
     for (int t = across ? kSliceTiles - 1 : 0; t < kSliceTiles; ++t) {
         const int a = kSlices[t].rows, n = gated ? kSlices[t].gated : kSlices[t].channels, b = gated ? 2 * n : n;
+        if (tiles(a, n) > kMaxSliceTiles) continue;
         const double count = tiles(a, n) / cus;
         const int together = 160 / (a + b);  // workgroups whose LDS a CU holds
         const double rounds = together >= 2 ? std::max(1.0, count) : std::ceil(count);
         const double one = std::max((a + b) * row / 80e3, eb == 4 ? a * b * row / eb / 500e3 : 0.0);
         const double time = (a + b >= 128 ? 4.6 : a + b >= 96 ? 3.8 : 3.4) + rounds * one;
-        if (time < least) least = time, best = t;
+        if (time < best.time) best = Choice{t, time};
     }
     if (product_tiles_ok(bits8, out, p)) {
         const double stages = std::ceil(row / 128);
-        const bool whole = product_pieces_ok(form, p, eb);
-        for (int wide = 0; wide <= (whole ? 1 : 0); ++wide) {
+        const int widths = product_pieces_ok(form, p, eb) ? 2 : 1;
+        for (int wide = 0; wide < widths; ++wide) {
             const int n = (wide ? 256 : 128) / (gated ? 2 : 1);
             const double time = (wide ? 8 : 6) + std::ceil(tiles(256, n) / cus) * stages * (wide ? 1.3 : 0.95);
-            if (time < least) least = time, best = kSliceTiles + wide;
+            if (time < best.time) best = Choice{kSliceTiles + wide, time};
         }
     }
-    if (best < kSliceTiles) return launch_product_slices(form, bits8, out, best, p, s);
-    return launch_product_tiles(form, bits8, out, best > kSliceTiles, p, s);
+    return best;
+}
+
+rtoss_status launch_chosen(int kernel, ProductForm form, bool bits8, rtoss_dtype out, const Product& p, hipStream_t s)
+{
+    if (kernel < kSliceTiles) return launch_product_slices(form, bits8, out, kernel, p, s);
+    return launch_product_tiles(form, bits8, out, kernel > kSliceTiles, p, s);
+}
+
+// A launch has at most kMaxSliceTiles of the largest slices: more rows than that take several.
+rtoss_status launch_product(ProductForm form, bool bits8, rtoss_dtype out, const Product& p, hipStream_t s)
+{
+    DeviceInfo dev;
+    RTOSS_TRY(current_device(&dev));
+    const int eb = bits8 ? 1 : elem_bytes(out), out_eb = elem_bytes(out);
+    const int64_t across = ((int64_t)p.N + 31) / 32 * 2;
+    const int64_t most = std::max<int64_t>(kMaxSliceTiles / across, 1) * 64;  // rows
+    if (p.M <= most) return launch_chosen(choose(form, bits8, out, p, dev.cus).kernel, form, bits8, out, p, s);
+    for (int64_t m = 0; m < p.M; m += most) {
+        Product part = p;
+        const auto on = [](const void* base, int64_t bytes) { return base ? (void*)((char*)base + bytes) : nullptr; };
+        const int64_t a_step = form == kBackWeights ? eb : p.lda * eb;  // (there the rows of the result are columns of its operand)
+        part.M = (int)std::min<int64_t>(most, p.M - m);
+        part.a0 = on(p.a0, m * a_step);
+        part.a1 = on(p.a1, m * a_step);
+        part.sa = (const float*)on(p.sa, m * 4);
+        part.residual = on(p.residual, m * p.ldr * out_eb);
+        part.y = on(p.y, m * p.ldy * out_eb);
+        part.y0 = on(p.y0, m * p.N * out_eb);
+        part.y1 = on(p.y1, m * (form == kBackWeights ? p.ldy : p.N) * out_eb);
+        RTOSS_TRY(launch_chosen(choose(form, bits8, out, part, dev.cus).kernel, form, bits8, out, part, s));
+    }
+    return RTOSS_OK;
+}
+
+// Both gradients, or one (the other's y is NULL), by the same kernels either way: in one launch of slices where that is shorter than two.
+//   one launch: 3.5 us, then 65 KB/us and CU for the rows of both operands, or the longest sum, four stages at a time (0.6 and 0.75 us for tiles of
+//   16 and 64 rows).  bf16 1024 -> 2752, rows 16, 128, 512, 2048, both gradients with dg and du: 18, 21, 32, 78 us, in two launches 40, 44, 42, 82.
+rtoss_status launch_gradients(rtoss_dtype dt, Product rows, Product weights, hipStream_t s)
+{
+    DeviceInfo dev;
+    RTOSS_TRY(current_device(&dev));
+    const int eb = elem_bytes(dt);
+    const auto up = [](int64_t n, int by) { return (double)((n + by - 1) / by); };
+    double two = choose(kBackWeights, false, dt, weights, dev.cus).time;
+    if (rows.M > 0) two += choose(kBackRows, false, dt, rows, dev.cus).time;
+    const double weight_tiles = 2 * up(weights.M, 64) * up(weights.N, 64), stages = std::ceil(rows.R * eb / 128.0) * 2;
+    bool high = false;
+    double one = 1e300;
+    for (int t = 0; t < 2; ++t) {
+        const int a = t ? 64 : 16;
+        const double row_tiles = up(rows.M, a) * up(rows.N, 64);
+        if (row_tiles + weight_tiles > kMaxSliceTiles) continue;
+        const double bytes = row_tiles * (a + 64) * 2.0 * rows.R * eb + weight_tiles * 128.0 * weights.R * eb;
+        const double time = 3.5 + std::max(std::ceil(stages / 4) * (t ? 0.75 : 0.6), bytes / (65e3 * dev.cus));
+        if (time < one) one = time, high = t;
+    }
+    if (one < two) return launch_product_slices_back(dt, high, rows, weights, s);
+    if (rows.y) RTOSS_TRY(launch_product(kBackRows, false, dt, rows, s));
+    if (weights.y) RTOSS_TRY(launch_product(kBackWeights, false, dt, weights, s));
+    return RTOSS_OK;
 }
 
 size_t slopes_bytes(const rtoss_gated_desc& d) { return align_up((size_t)d.M * slopes_pitch(d.F, d.dt) * elem_bytes(d.dt), 256); }
@@ -313,29 +374,22 @@ rtoss_status rtoss_gated_ff_backward(const rtoss_gated_desc* desc, const void* d
     p.a0 = dg;
     p.a1 = du;
     p.lda = slopes_pitch(d.F, d.dt);
-    if (rows) {
-        p.b0 = w_gate_dev;
-        p.b1 = w_up_dev;
-        p.ldb = d.w_ld;
-        p.M = (int)d.M;
-        p.N = d.K;
-        p.R = d.F;
-        p.y = dx_dev;
-        p.ldy = d.K;
-        RTOSS_TRY(launch_product(kBackRows, false, d.dt, p, s));
-    }
-    if (weights) {
-        p.b0 = x_dev;
-        p.ldb = d.x_ld;
-        p.M = d.F;
-        p.N = d.K;
-        p.R = (int)d.M;
-        p.y = dw_gate_dev;
-        p.y1 = dw_up_dev;
-        p.ldy = d.K;
-        RTOSS_TRY(launch_product(kBackWeights, false, d.dt, p, s));
-    }
-    return RTOSS_OK;
+    p.N = d.K;
+    p.ldy = d.K;
+    Product to_rows = p, to_weights = p;
+    to_rows.b0 = w_gate_dev;
+    to_rows.b1 = w_up_dev;
+    to_rows.ldb = d.w_ld;
+    to_rows.M = (int)d.M;
+    to_rows.R = d.F;
+    to_rows.y = rows ? dx_dev : nullptr;
+    to_weights.b0 = x_dev;
+    to_weights.ldb = d.x_ld;
+    to_weights.M = d.F;
+    to_weights.R = (int)d.M;
+    to_weights.y = dw_gate_dev;
+    to_weights.y1 = dw_up_dev;
+    return launch_gradients(d.dt, to_rows, to_weights, s);
 }
 
 }  // extern "C"

@@ -542,6 +542,20 @@ def test_offsets_past_32_bits():
     equal(dwu, (du.t() @ x.double()).to(torch.bfloat16))
 
 
+def test_more_rows_than_a_launch_takes():
+    """140 million rows of one channel: more tiles than one launch has."""
+    g = gen(71)
+    M = 140_000_000
+    a = codes(g, (M, 1))
+    w = codes(g, (1, 1))
+    s = torch.ones(M, device="cuda")
+    s[-7:] = torch.arange(7, device="cuda").float()
+    y = pl.matmul_i8(a, s, w, None, out_dt=B.F32)
+    for at in (slice(0, 1000), slice(M - 1000, M), slice(134_217_000, 134_219_000)):
+        equal(y[at], a[at].float() * w.float() * s[at, None])
+    assert torch.equal(y, a.float() * w.float() * s[:, None])
+
+
 def test_refusals_of_tensors():
     x, w = torch.zeros(4, 16, device="cuda"), torch.zeros(8, 16, device="cuda")
     q, s = pl.quantize_rows(x)
