@@ -79,6 +79,8 @@ __device__ __forceinline__ void copy16_bounded(__amdgpu_buffer_rsrc_t from, uint
 //   kWhole  pieces of 16 bytes start at multiples of 16 bytes: copies
 //   kWords  ... at multiples of 4: through registers
 //   kBytes  ... anywhere: through registers, with the word behind (a load of 16 bytes that is not aligned to a word takes 64 cycles instead of 16)
+typedef uint32_t u32x4_words __attribute__((ext_vector_type(4), aligned(4)));  // on words
+
 enum Rows { kWhole = 0, kWords, kBytes };
 
 // 16 bytes at p; kBytes: in two parts
@@ -90,7 +92,7 @@ template <int ROWS> struct Piece {
         if constexpr (ROWS == kBytes) {
             const uint32_t shift = (uint32_t)(uintptr_t)p & 3;
             const char* word = p - shift;
-            v = *(const __attribute__((aligned(4))) u32x4*)word;
+            v = *(const u32x4_words*)word;
             behind = *(const uint32_t*)(word + (shift ? 16 : 12));  // (only words that hold a byte of the piece)
         } else {
             __builtin_memcpy(&v, __builtin_assume_aligned(p, 4), 16);
