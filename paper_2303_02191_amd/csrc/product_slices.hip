@@ -10,6 +10,7 @@
 #include "fp32_split.h"
 #include "product_run.h"
 #include "product_tile.h"
+#include "product_words.h"
 
 namespace rtoss {
 
@@ -218,134 +219,35 @@ __device__ __forceinline__ void product_slices(Product p, int work, int tiles_m,
             });
         }
     } else {
-        // ---- through registers: a stage is loaded while the one before is multiplied.  (One wave's LDS instructions run in their order.)  Rows that
-        // do not begin on words (kBytes): pieces of whole words, of which a lane's last bytes are the next lane's first word; that behind the last
-        // piece of a row comes from a load of its own, one for eight instructions.  (A fifth word for every piece: 16 registers more at 64 x 64, which
-        // spilled; 8-bit 512 x 4091 x 4096 FIFTH us, now THIS.) ----
-        constexpr int E = 16 / EB;
-        constexpr int ENDS = ROWS == kBytes ? (PIECES + 7) / 8 : 0;
-        static_assert(ROWS != kBytes || EB < 4, "fp32 rows begin on words");
-        u32x4 piece_in[PIECES];
-        uint32_t end_in[ENDS ? ENDS : 1];
-        constexpr int PA = A_ACROSS ? AcrossA::kPieces : 8, PB = B_ACROSS ? AcrossB::kPieces : 8;  // pieces of a row in a stage
-        constexpr int TILES = GATED ? NT / 2 : NT;
-        auto is_a = [](int i) { return i < A_COPIES; };
-        auto row_in = [&](int i, int lane) { return is_a(i) ? i * (64 / PA) + lane / PA : (i - A_COPIES) * (64 / PB) + lane / PB; };  // of instruction i
-        auto piece_of = [&](int i, int lane) { return is_a(i) ? lane % PA : lane % PB; };
-        auto channel = [&](int i, int lane) {
-            const int rho = row_in(i, lane), in = rho % COLS;
-            return 4 * TILES * ((in & 15) >> 2) + 4 * (in / 16) + (in & 3);
-        };
-        auto base_of = [&](int i, int st) {
-            const bool second = FORM == kBackRows && st >= S1;
-            if (is_a(i)) return (const char*)(second ? p.a1 : p.a0) + (A_ACROSS ? m0 * EB : m0 * lda);
-            return (const char*)(second || (GATED && i - A_COPIES >= B_COPIES / 2) ? p.b1 : p.b0) + (B_ACROSS ? (int64_t)n0 * EB : n0 * ldb);
-        };
-        auto in_pair = [&](int st) { return FORM == kBackRows && st >= S1 ? st - S1 : st; };
-
-        // Where all pieces of a stage can be loaded whole: an offset from the tile that does not change, the stage moves a uniform base.  (Rows past
-        // the last are the last again.  Across, columns past the last are what lies behind, in the row after: not the last one's.)
-        const bool near = lda <= 1 << 24 && ldb <= 1 << 24;  // (of further rows every piece is found by itself)
-        auto inside = [&](int stage) {                       // uniform
-            const int64_t end = (in_pair(stage) + 1) * (int64_t)STAGE;
-            constexpr int BEHIND = ROWS == kBytes ? 36 : 16;
-            return near && (A_ACROSS || B_ACROSS ? end < p.R && (!A_ACROSS || lda >= BEHIND) && ldb >= BEHIND : end <= p.R);
-        };
-        auto near_row = [&](int i) {  // offset of the row
-            const uint32_t ld = (uint32_t)(is_a(i) ? lda : ldb);
-            if (is_a(i) ? A_ACROSS : B_ACROSS) return row_in(i, lane) * ld;
-            return (is_a(i) ? (uint32_t)min((int64_t)row_in(i, lane), p.M - 1 - m0) : (uint32_t)min(channel(i, lane), p.N - 1 - n0)) * ld;
-        };
-        auto near_piece = [&](int i, int piece) {  // of the piece in its row; kBytes: also of the one behind the last that exists
-            if (!(is_a(i) ? A_ACROSS : B_ACROSS)) return piece * 16;
-            const int last = (int)min(is_a(i) ? p.M - m0 : (int64_t)(p.N - n0), (int64_t)64) - 1;
-            return min(piece, last / E + (ROWS == kBytes)) * 16;
-        };
-        uint32_t at_piece[PIECES], at_end[ENDS ? ENDS : 1];
-#pragma unroll
-        for (int i = 0; i < PIECES; ++i) at_piece[i] = near_row(i) + near_piece(i, piece_of(i, lane));
-        auto end_of = [&](int j, int lane) { return min(8 * j + (lane & 7), PIECES - 1); };  // whose row's end this lane loads
-#pragma unroll
-        for (int j = 0; j < ENDS; ++j) at_end[j] = near_row(end_of(j, lane)) + near_piece(end_of(j, lane), 8) - 1;
-        auto stage_base = [&](int i, int stage) {
-            const int st = in_pair(stage);
-            return base_of(i, stage) + ((is_a(i) ? A_ACROSS : B_ACROSS) ? (int64_t)st * STAGE * (is_a(i) ? lda : ldb) : (int64_t)st * kStage);
-        };
-        // Otherwise, words from `first` on of a row (which exists), those past its last being that one again
-        struct Words {
-            const uint32_t* at;
-            int more;
-            __device__ __forceinline__ uint32_t operator[](int w) const { return at[min(w, more)]; }
-        };
-        auto words = [&](int i, int lane, int stage, int piece, int& have) {
-            const int st = in_pair(stage);
-            const bool across = is_a(i) ? A_ACROSS : B_ACROSS;
-            const int64_t ld = is_a(i) ? lda : ldb;
-            const int64_t r = across ? (int64_t)st * STAGE + row_in(i, lane)
-                              : is_a(i) ? min((int64_t)row_in(i, lane), p.M - 1 - m0) : (int64_t)min(channel(i, lane), p.N - 1 - n0);
-            const int64_t columns = across ? (is_a(i) ? p.M - m0 : (int64_t)p.N - n0) : p.R;
-            const int64_t from = (across ? 0 : (int64_t)st * STAGE) + piece * E;
-            have = across && r >= p.R ? 0 : (int)min((int64_t)E, columns - from);
-            const uintptr_t in_row = (uintptr_t)base_of(i, stage) + (across ? min(r, (int64_t)p.R - 1) : r) * ld;
-            const int64_t last = (int64_t)(columns * EB + (in_row & 3) - 1) >> 2, first = min(from * EB >> 2, last);
-            return Words{(const uint32_t*)(in_row & ~(uintptr_t)3) + first, (int)min(last - first, (int64_t)4)};
-        };
-        auto load = [&](int st) {
-            if (inside(st)) {
-#pragma unroll
-                for (int i = 0; i < PIECES; ++i) {
-                    const char* at = stage_base(i, st) + at_piece[i];
-                    if constexpr (ROWS == kBytes) at -= (uintptr_t)at & 3;
-                    piece_in[i] = *(const u32x4_words*)at;
-                }
-#pragma unroll
-                for (int j = 0; j < ENDS; ++j) {
-                    const char* at = stage_base(end_of(j, lane), st) + at_end[j];
-                    end_in[j] = *(const uint32_t*)(at - ((uintptr_t)at & 3));
-                }
-            } else {
-                int have, here = lane;
-                asm volatile("" : "+v"(here));  // (nothing of this is worth a register in the loop)
-#pragma unroll
-                for (int i = 0; i < PIECES; ++i) {
-                    const Words from = words(i, here, st, piece_of(i, here), have);
-#pragma unroll
-                    for (int w = 0; w < 4; ++w) piece_in[i][w] = from[w];
-                }
-#pragma unroll
-                for (int j = 0; j < ENDS; ++j) end_in[j] = words(end_of(j, here), here, st, 7, have)[4];
+        // ---- through registers: a stage is loaded while the one before is multiplied.  (One wave's LDS instructions run in their order.) ----
+        constexpr int PA = A_ACROSS ? AcrossA::kPieces : 8, PB = B_ACROSS ? AcrossB::kPieces : 8;
+        struct Place {
+            char* own;
+            int lane;
+            static __device__ __forceinline__ int row(int i, int lane)
+            {
+                const bool of_a = i < A_COPIES;
+                const int k = of_a ? i : i - A_COPIES, r = of_a ? k * (64 / PA) + lane / PA : k * (64 / PB) + lane / PB;
+                if (of_a || B_ACROSS) return r;
+                constexpr int TILES = GATED ? NT / 2 : NT;
+                const int in = r % COLS;
+                return 4 * TILES * ((in & 15) >> 2) + 4 * (in / 16) + (in & 3);
+            }
+            static __device__ __forceinline__ int column(int) { return 0; }
+            static __device__ __forceinline__ bool up(int i) { return GATED && i - A_COPIES >= B_COPIES / 2; }
+            __device__ __forceinline__ char* to(int i, int) const
+            {
+                const int k = i < A_COPIES ? i : i - A_COPIES;
+                const int spread = (i < A_COPIES ? A_ACROSS : B_ACROSS) ? AcrossA::spread(k * AcrossA::kCopyRows + lane / AcrossA::kPieces) : lane >> 3;
+                return own + (i < A_COPIES ? 0 : A_BYTES) + k * 1024 + (lane ^ spread) * 16;
             }
         };
-        auto store = [&](int st) {
-            const bool whole_pieces = inside(st);
-            static_for<PIECES>([&](auto which) {
-                constexpr int i = which;
-                constexpr bool across = i < A_COPIES ? A_ACROSS : B_ACROSS;
-                u32x4 v = piece_in[i];
-                if constexpr (ROWS == kBytes) {
-                    // (rows of an instruction are eight apart from those of the next, or, of B's, a number of whole channels of four)
-                    const uint32_t shift = (uint32_t)(uintptr_t)base_of(i, st) + (uint32_t)(lane >> 3 & 3) * (uint32_t)(i < A_COPIES ? lda : ldb);
-                    const uint32_t next = __builtin_amdgcn_update_dpp(0, v[0], 0x101, 0xf, 0xf, true);  // the next lane's
-                    uint32_t end = end_in[i / 8];
-                    if constexpr (i % 8 != 7) end = __builtin_amdgcn_update_dpp(0, end, 0x110 + 7 - i % 8, 0xf, 0xf, true);
-                    const uint32_t behind = (lane & 7) == 7 ? end : next;
-                    v = u32x4{__builtin_amdgcn_alignbyte(v[1], v[0], shift), __builtin_amdgcn_alignbyte(v[2], v[1], shift),
-                              __builtin_amdgcn_alignbyte(v[3], v[2], shift), __builtin_amdgcn_alignbyte(behind, v[3], shift)};
-                }
-                if (!whole_pieces) {  // words that do not exist: other ones, cut off here
-                    int have, here = lane;
-                    asm volatile("" : "+v"(here));
-                    (void)words(i, here, st, piece_of(i, here), have);
-                    keep_first<T>(v, have);
-                }
-                const int k = i < A_COPIES ? i : i - A_COPIES, spread = across ? AcrossA::spread(row_in(i, lane)) : lane >> 3;
-                *(u32x4*)(own + (i < A_COPIES ? 0 : A_BYTES) + k * 1024 + (lane ^ spread) * 16) = v;
-            });
-        };
-        if (wave < S) load(wave);
+        const Place place{own, lane};
+        StageInRegisters<T, FORM, ROWS, PIECES, A_COPIES, PA, PB, Place> in_registers(p, place, m0, n0, S1, lane);
+        if (wave < S) in_registers.load(wave);
         for (int s = wave; s < S; s += WAVES) {
-            store(s);
-            if (s + WAVES < S) load(s + WAVES);
+            in_registers.store(s);
+            if (s + WAVES < S) in_registers.load(s + WAVES);
             fence();
             read_and_multiply(own, s, [&] {});
             fence();

@@ -79,45 +79,9 @@ __device__ __forceinline__ void copy16_bounded(__amdgpu_buffer_rsrc_t from, uint
 //   kWhole  pieces of 16 bytes start at multiples of 16 bytes: copies
 //   kWords  ... at multiples of 4: through registers
 //   kBytes  ... anywhere: through registers, with the word behind (a load of 16 bytes that is not aligned to a word takes 64 cycles instead of 16)
-typedef uint32_t u32x4_words __attribute__((ext_vector_type(4), aligned(4)));  // on words
-
 enum Rows { kWhole = 0, kWords, kBytes };
 
-// 16 bytes at p; kBytes: in two parts
-template <int ROWS> struct Piece {
-    u32x4 v;
-    uint32_t behind;
-    __device__ __forceinline__ void load(const char* p)
-    {
-        if constexpr (ROWS == kBytes) {
-            const uint32_t shift = (uint32_t)(uintptr_t)p & 3;
-            const char* word = p - shift;
-            v = *(const u32x4_words*)word;
-            behind = *(const uint32_t*)(word + (shift ? 16 : 12));  // (only words that hold a byte of the piece)
-        } else {
-            __builtin_memcpy(&v, __builtin_assume_aligned(p, 4), 16);
-        }
-    }
-    // of which only `bytes` exist, at least one: words past the last of them repeat it
-    __device__ __forceinline__ void load_part(const char* p, int bytes)
-    {
-        const uint32_t shift = ROWS == kBytes ? (uint32_t)(uintptr_t)p & 3 : 0;
-        const uint32_t* word = (const uint32_t*)(p - shift);
-        const int last = (min(bytes, 16) + (int)shift - 1) >> 2;
-#pragma unroll
-        for (int w = 0; w < 4; ++w) v[w] = word[min(w, last)];
-        if constexpr (ROWS == kBytes) behind = word[last];
-    }
-    __device__ __forceinline__ u32x4 value(uint32_t shift) const
-    {
-        if constexpr (ROWS == kBytes) {
-            return u32x4{__builtin_amdgcn_alignbyte(v[1], v[0], shift), __builtin_amdgcn_alignbyte(v[2], v[1], shift),
-                         __builtin_amdgcn_alignbyte(v[3], v[2], shift), __builtin_amdgcn_alignbyte(behind, v[3], shift)};
-        } else {
-            return v;
-        }
-    }
-};
+typedef uint32_t u32x4_words __attribute__((ext_vector_type(4), aligned(4)));  // on words
 
 // kWhole, kWords or kBytes for operands of `eb`-byte elements.
 inline Rows product_rows(ProductForm form, const Product& p, int eb)

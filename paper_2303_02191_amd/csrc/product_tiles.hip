@@ -28,6 +28,7 @@
 
 #include "product_run.h"
 #include "product_tile.h"
+#include "product_words.h"
 
 namespace rtoss {
 
@@ -89,13 +90,33 @@ __global__ __launch_bounds__(512, 2) void product_tiles_kernel(Product p, int ti
     // A lane's channel is such that its results are neighbouring channels ----
     const int sub = lane >> 3, piece = (lane & 7) ^ sub;
     constexpr int PIECES = Across<T, 128>::kPieces, COPY_ROWS = Across<T, 128>::kCopyRows;
-    // a region's row of B -> channel of the tile (gated: runs of 8 channels a lane in 32 of a wave; otherwise of 16 in 64, of which a region
-    // has half where there are two, the second 8 channels on)
-    auto channel = [](int rho) {
-        const int r = rho & 15, tile = rho >> 4;
-        if constexpr (GATED) return (tile * 16 & COLS - 1) / 32 * 32 + 8 * (r >> 2) + 4 * (tile & 1) + (r & 3);
-        else if constexpr (B_REGIONS == 2) return (tile >> 1) * 64 + 16 * (r >> 2) + 4 * (tile & 1) + (r & 3);
-        else return (tile >> 2) * 64 + 16 * (r >> 2) + 4 * (tile & 3) + (r & 3);
+    struct Place {  // of a lane's pieces: 0 .. 3 of A's halves, 4 and 5 of B
+        char* smem;
+        int wave, lane;
+        bool late;
+        // a region's row of B -> channel of the tile (gated: runs of 8 channels a lane in 32 of a wave; otherwise of 16 in 64, of which a region
+        // has half where there are two, the second 8 channels on)
+        static __device__ __forceinline__ int channel(int rho)
+        {
+            const int r = rho & 15, tile = rho >> 4;
+            if constexpr (GATED) return (tile * 16 & COLS - 1) / 32 * 32 + 8 * (r >> 2) + 4 * (tile & 1) + (r & 3);
+            else if constexpr (B_REGIONS == 2) return (tile >> 1) * 64 + 16 * (r >> 2) + 4 * (tile & 1) + (r & 3);
+            else return (tile >> 2) * 64 + 16 * (r >> 2) + 4 * (tile & 3) + (r & 3);
+        }
+        static __device__ __forceinline__ bool of_a(int i) { return i < 4; }
+        __device__ __forceinline__ int row(int i, int lane) const
+        {
+            if (of_a(i) ? A_ACROSS : B_ACROSS) return (wave * 2 + i % 2) * COPY_ROWS + lane / PIECES;
+            const int rho = wave * 16 + i % 2 * 8 + lane / 8;
+            return of_a(i) ? i / 2 * 128 + rho : channel(rho);
+        }
+        static __device__ __forceinline__ int column(int i) { return of_a(i) ? i / 2 * 128 : 0; }
+        __device__ __forceinline__ bool up(int i) const { return GATED && !of_a(i) && late; }
+        __device__ __forceinline__ char* to(int i, int stage) const
+        {
+            const int spread = (of_a(i) ? A_ACROSS : B_ACROSS) ? Across<T, 128>::spread((wave * 2 + i % 2) * COPY_ROWS + lane / PIECES) : lane >> 3;
+            return smem + (stage & 1) * kBuffer + i / 2 * kRegion + wave * 2048 + i % 2 * 1024 + (lane ^ spread) * 16;
+        }
     };
     uint32_t va[2], vb[2];
 #pragma unroll
@@ -107,7 +128,7 @@ __global__ __launch_bounds__(512, 2) void product_tiles_kernel(Product p, int ti
         if constexpr (B_ACROSS) {
             vb[i] = (uint32_t)r_across * (uint32_t)ldb + at_across;
         } else {
-            vb[i] = (uint32_t)channel(rho) * (uint32_t)ldb + piece * 16;
+            vb[i] = (uint32_t)Place::channel(rho) * (uint32_t)ldb + piece * 16;
         }
     }
     // kind: 0, 1 halves of A; 2, 3 regions of B.  Gated with one region: w_gate's rows, then w_up's, which are the upper waves' to copy
@@ -135,60 +156,10 @@ __global__ __launch_bounds__(512, 2) void product_tiles_kernel(Product p, int ti
     };
 
     // ---- rows that are no whole pieces: through registers, a stage's six pieces of a lane at once ----
-    constexpr int E = 16 / EB, KINDS = 2 + B_REGIONS;
     static_assert(ROWS == kWhole || B_REGIONS == 1, "the second region's channels");
-    Piece<ROWS> piece_in[ROWS == kWhole ? 1 : 2 * KINDS];
-    // piece i of region `kind`: its address, and how many of its elements exist
-    auto place = [&](int kind, int i, int stage, int& have) {
-        int st = stage;
-        const bool second = FORM == kBackRows && st >= S1;
-        if (second) st -= S1;
-        const bool of_a = kind < 2;
-        const int64_t ld = of_a ? lda : ldb;
-        if (of_a ? A_ACROSS : B_ACROSS) {
-            const int r = (wave * 2 + i) * COPY_ROWS + lane / PIECES;
-            const int64_t row_at = (int64_t)st * STAGE + r;
-            const int64_t column = (of_a ? m0 + kind * 128 : n0) + (lane % PIECES ^ Across<T, 128>::spread(r)) * E;
-            have = row_at < p.R ? (int)min((int64_t)E, (of_a ? p.M : p.N) - column) : 0;
-            return (const char*)(of_a ? p.a0 : second ? p.b1 : p.b0) + row_at * ld + column * EB;
-        }
-        const int rho = wave * 16 + i * 8 + sub, r_at = st * STAGE + piece * E;
-        have = min(E, p.R - r_at);
-        if (of_a) return (const char*)(second ? p.a1 : p.a0) + min(m0 + kind * 128 + rho, (int64_t)p.M - 1) * ld + (int64_t)r_at * EB;
-        return (const char*)(GATED && late ? p.b1 : p.b0) + (int64_t)min(n0 + channel(rho), p.N - 1) * ld + (int64_t)r_at * EB;
-    };
-    auto inside = [&](int stage) {  // every piece of the stage is whole: uniform
-        const int st = FORM == kBackRows && stage >= S1 ? stage - S1 : stage;
-        return (st + 1) * (int64_t)STAGE <= p.R && (!A_ACROSS || m0 + kTileM <= p.M) && (!B_ACROSS || n0 + TILE_N <= p.N);
-    };
-    auto load = [&](int stage) {
-        if (inside(stage)) {
-#pragma unroll
-            for (int k = 0; k < 2 * KINDS; ++k) {
-                int have;
-                piece_in[k].load(place(k / 2, k % 2, stage, have));
-            }
-        } else {
-#pragma unroll
-            for (int k = 0; k < 2 * KINDS; ++k) {
-                int have;
-                const char* at = place(k / 2, k % 2, stage, have);
-                piece_in[k].load_part(have > 0 ? at : (const char*)(k < 4 ? p.a0 : p.b0), have > 0 ? have * EB : 1);
-            }
-        }
-    };
-    auto store = [&](int stage) {
-        const bool whole_stage = inside(stage);
-#pragma unroll
-        for (int k = 0; k < 2 * KINDS; ++k) {
-            int have;
-            const char* at = place(k / 2, k % 2, stage, have);
-            u32x4 v = piece_in[k].value((uint32_t)(uintptr_t)at);  // (words that do not exist: other ones, cut off here)
-            if (!whole_stage) keep_first<T>(v, have);
-            *(u32x4*)(smem + (stage & 1) * kBuffer + k / 2 * kRegion + wave * 2048 + k % 2 * 1024 + lane * 16) = v;
-        }
-    };
-
+    constexpr int PA = A_ACROSS ? PIECES : 8, PB = B_ACROSS ? PIECES : 8;
+    const Place place{smem, wave, lane, late};
+    StageInRegisters<T, FORM, ROWS == kWhole ? kWords : ROWS, 6, 4, PA, PB, Place> in_registers(p, place, m0, n0, S1, lane);
     Acc acc[2 * MT][4];
 #pragma unroll
     for (int i = 0; i < 8 * MT; ++i) acc[i >> 2][i & 3] = Acc{0, 0, 0, 0};
@@ -257,10 +228,10 @@ __global__ __launch_bounds__(512, 2) void product_tiles_kernel(Product p, int ti
         issue_first(0), issue(0, 1), issue_first(1);
     } else {
         if (S > 0) {  // (a sum of nothing has no memory behind its operands)
-            load(0);
-            store(0);
+            in_registers.load(0);
+            in_registers.store(0);
         }
-        if (S > 1) load(1);
+        if (S > 1) in_registers.load(1);
     }
     landed();
     meet();
@@ -285,8 +256,8 @@ __global__ __launch_bounds__(512, 2) void product_tiles_kernel(Product p, int ti
         if constexpr (ROWS == kWhole) {
             issue_first(s + 2);
         } else if (s + 1 < S) {  // (the other buffer has been read: both groups of waves are past a barrier behind its last part)
-            store(s + 1);
-            if (s + 2 < S) load(s + 2);
+            in_registers.store(s + 1);
+            if (s + 2 < S) in_registers.load(s + 2);
         }
         landed();
         meet();
