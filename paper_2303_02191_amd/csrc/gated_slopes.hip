@@ -32,12 +32,15 @@ template <typename T, int ACT> __device__ __forceinline__ void slopes(float g, f
 // rows of the inputs, without gaps.
 template <typename T, int ACT, bool VEC>
 __global__ __launch_bounds__(256) void gated_slopes_kernel(const T* __restrict__ dh, const T* __restrict__ gate, const T* __restrict__ up,
-                                                           T* __restrict__ dg, T* __restrict__ du, int64_t pieces, int per_row, int F, int64_t ldh)
+                                                           T* __restrict__ dg, T* __restrict__ du, int64_t pieces, int per_row, int F, int64_t ldh,
+                                                           uint32_t* __restrict__ counters, int counts)
 {
     constexpr int E = 16 / (int)sizeof(T);
     // VEC: one run of pieces; otherwise a row of workgroups for each row (or every gridDim.y-th), so that there is none to find
     const int64_t step = VEC ? (int64_t)gridDim.x * 256 : per_row * (int64_t)gridDim.y;
     const int at = (int)blockIdx.x * 256 + (int)threadIdx.x;
+    if (blockIdx.y == 0)
+        for (int i = at; i < counts; i += (int)gridDim.x * 256) counters[i] = 0;
     if (!VEC && at >= per_row) return;
     int64_t m = blockIdx.y;
     for (int64_t i = VEC ? at : m * per_row + at; i < pieces; i += step, m += gridDim.y) {
@@ -74,7 +77,8 @@ __global__ __launch_bounds__(256) void gated_slopes_kernel(const T* __restrict__
 }
 
 template <typename T>
-rtoss_status launch(rtoss_act act, int64_t M, int F, const void* dh, int64_t ldh, const void* gate, const void* up, void* dg, void* du, hipStream_t s)
+rtoss_status launch(rtoss_act act, int64_t M, int F, const void* dh, int64_t ldh, const void* gate, const void* up, void* dg, void* du,
+                    uint32_t* counters, int counts, hipStream_t s)
 {
     constexpr int E = 16 / (int)sizeof(T);
     const bool vec = F % E == 0 && ldh == F && ((uintptr_t)dh | (uintptr_t)gate | (uintptr_t)up) % 16 == 0;
@@ -82,7 +86,7 @@ rtoss_status launch(rtoss_act act, int64_t M, int F, const void* dh, int64_t ldh
     const int64_t pieces = M * per_row;
     const dim3 grid = vec ? dim3((unsigned)std::min<int64_t>((pieces + 255) / 256, 16384)) : dim3((per_row + 255) / 256, (unsigned)std::min<int64_t>(M, 16384));
     auto go = [&](auto kernel) {
-        kernel<<<grid, 256, 0, s>>>((const T*)dh, (const T*)gate, (const T*)up, (T*)dg, (T*)du, pieces, per_row, F, ldh);
+        kernel<<<grid, 256, 0, s>>>((const T*)dh, (const T*)gate, (const T*)up, (T*)dg, (T*)du, pieces, per_row, F, ldh, counters, counts);
         return check_hip(hipGetLastError(), "gated_slopes launch");
     };
     switch (act) {
@@ -95,12 +99,12 @@ rtoss_status launch(rtoss_act act, int64_t M, int F, const void* dh, int64_t ldh
 }  // namespace
 
 rtoss_status launch_gated_slopes(rtoss_dtype dt, rtoss_act act, int64_t M, int F, const void* dh, int64_t ldh, const void* gate, const void* up,
-                                 void* dg, void* du, hipStream_t s)
+                                 void* dg, void* du, uint32_t* counters, int counts, hipStream_t s)
 {
     switch (dt) {
-    case RTOSS_F32: return launch<float>(act, M, F, dh, ldh, gate, up, dg, du, s);
-    case RTOSS_F16: return launch<f16_t>(act, M, F, dh, ldh, gate, up, dg, du, s);
-    default: return launch<bf16_t>(act, M, F, dh, ldh, gate, up, dg, du, s);
+    case RTOSS_F32: return launch<float>(act, M, F, dh, ldh, gate, up, dg, du, counters, counts, s);
+    case RTOSS_F16: return launch<f16_t>(act, M, F, dh, ldh, gate, up, dg, du, counters, counts, s);
+    default: return launch<bf16_t>(act, M, F, dh, ldh, gate, up, dg, du, counters, counts, s);
     }
 }
 

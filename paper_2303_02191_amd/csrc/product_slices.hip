@@ -16,9 +16,27 @@ namespace rtoss {
 
 namespace {
 
-// One tile of a product, `work` of tiles_m x tiles_n.
-template <typename T, typename TO, int FORM, int ROWS, int BM, int BN, int WAVES>
-__device__ __forceinline__ void product_slices(Product p, int work, int tiles_m, int tiles_n)
+// A long sum of few tiles is shared by `parts` workgroups: each leaves what it summed in memory, and the last of a tile's to arrive adds them, in their
+// order.  What crosses XCDs is written and read by atomic operations of the device's scope, past the L2s, with a wait in front of the count; a fence
+// of that scope would write back all of an L2.
+__device__ __forceinline__ void put_part(f32x4* at, f32x4 v)
+{
+    typedef uint64_t u64x2 __attribute__((ext_vector_type(2)));
+    const u64x2 halves = __builtin_bit_cast(u64x2, v);
+    __hip_atomic_store((uint64_t*)at, halves[0], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __hip_atomic_store((uint64_t*)at + 1, halves[1], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ f32x4 get_part(const f32x4* at)
+{
+    typedef uint64_t u64x2 __attribute__((ext_vector_type(2)));
+    const u64x2 halves = {__hip_atomic_load((const uint64_t*)at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT),
+                          __hip_atomic_load((const uint64_t*)at + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)};
+    return __builtin_bit_cast(f32x4, halves);
+}
+
+// One tile of a product, or a part of its sum: `work` of tiles_m x tiles_n x sum.parts.
+template <typename T, typename TO, int FORM, int ROWS, int BM, int BN, int WAVES, bool PARTS = false>
+__device__ __forceinline__ void product_slices(Product p, int work, int tiles_m, int tiles_n, SumParts sum_parts = {1, nullptr, nullptr})
 {
     typedef typename AccOf<T>::type Acc;
     constexpr bool GATED = FORM == kGated;
@@ -34,6 +52,8 @@ __device__ __forceinline__ void product_slices(Product p, int work, int tiles_m,
     const int c = lane & 15, q = lane >> 4;
 
     // in groups of eight row tiles, rows fastest: the workgroups that run on an XCD at a time share rows and channels in its L2
+    const int part = PARTS ? work / (tiles_m * tiles_n) : 0;
+    if constexpr (PARTS) work -= part * (tiles_m * tiles_n);
     constexpr int GROUP = 8;
     const int group = work / (GROUP * tiles_n), in_group = work - group * (GROUP * tiles_n);
     const int high = min(GROUP, tiles_m - group * GROUP);
@@ -52,6 +72,7 @@ __device__ __forceinline__ void product_slices(Product p, int work, int tiles_m,
     const int64_t lda = p.lda * EB, ldb = p.ldb * EB, row = (int64_t)p.R * EB;
     const int S1 = (int)(((int64_t)p.R + STAGE - 1) / STAGE), S = FORM == kBackRows ? 2 * S1 : S1;
     const int rest = p.R - (S1 - 1) * STAGE;  // rows of the sum in the last stage
+    const int begin = PARTS ? (int)((int64_t)S * part / sum_parts.parts) : 0, end = PARTS ? (int)((int64_t)S * (part + 1) / sum_parts.parts) : S;
     auto whole = [](int64_t bytes) { return (bytes + 15) & ~(int64_t)15; };  // (dg and du, whose rows are padded)
     auto rows_from = [&](const void* base, int64_t ld, int64_t first, int64_t rows) {
         return Source{(const char*)base + first * ld, (rows - 1 - first) * ld + whole(row)};
@@ -205,8 +226,8 @@ __device__ __forceinline__ void product_slices(Product p, int work, int tiles_m,
             const From f = source(s);
             static_for<PIECES>([&](auto k) { copy(f, lds0, k); });
         };
-        if (wave < S) issue(wave);
-        for (int s = wave; s < S; s += WAVES) {
+        if (begin + wave < end) issue(begin + wave);
+        for (int s = begin + wave; s < end; s += WAVES) {
             fence();
             __builtin_amdgcn_s_waitcnt(0x0f70);  // the stage has landed
             fence();
@@ -214,7 +235,7 @@ __device__ __forceinline__ void product_slices(Product p, int work, int tiles_m,
                 fence();
                 __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): its place is free
                 fence();
-                if (s + WAVES < S) issue(s + WAVES);
+                if (s + WAVES < end) issue(s + WAVES);
                 __builtin_amdgcn_sched_barrier(0);
             });
         }
@@ -244,10 +265,10 @@ __device__ __forceinline__ void product_slices(Product p, int work, int tiles_m,
         };
         const Place place{own, lane};
         StageInRegisters<T, FORM, ROWS, PIECES, A_COPIES, PA, PB, Place> in_registers(p, place, m0, n0, S1, lane);
-        if (wave < S) in_registers.load(wave);
-        for (int s = wave; s < S; s += WAVES) {
+        if (begin + wave < end) in_registers.load(begin + wave);
+        for (int s = begin + wave; s < end; s += WAVES) {
             in_registers.store(s);
-            if (s + WAVES < S) in_registers.load(s + WAVES);
+            if (s + WAVES < end) in_registers.load(s + WAVES);
             fence();
             read_and_multiply(own, s, [&] {});
             fence();
@@ -263,17 +284,24 @@ __device__ __forceinline__ void product_slices(Product p, int work, int tiles_m,
 #pragma unroll
         for (int n = 0; n < NT; ++n) joined[((wave * MT + i) * NT + n) * 64 + lane] = acc[i][n];
     __syncthreads();
-    auto finish = [&](int unit, const Output& out, float sa) {
-        const int64_t m = row_of(unit);
+    struct Sum {
+        Acc of[PART];
+    };
+    auto sum_of = [&](int unit) {
         const int share = unit % SHARE;
-        Acc sum[PART];
+        Sum sum;
 #pragma unroll
         for (int t = 0; t < PART; ++t) {
             const Acc* from = joined + (unit / SHARE * NT + (GATED ? NT / 2 * t + share : PART * share + t)) * 64 + lane;
-            sum[t] = from[0];
+            sum.of[t] = from[0];
 #pragma unroll
-            for (int w = 1; w < WAVES; ++w) sum[t] += from[w * MT * NT * 64];
+            for (int w = 1; w < WAVES; ++w) sum.of[t] += from[w * MT * NT * 64];
         }
+        return sum;
+    };
+    auto finish = [&](int unit, const Output& out, float sa, const Sum& of) {
+        const auto& sum = of.of;
+        const int64_t m = row_of(unit);
         if (m >= p.M) return;
 #pragma unroll
         for (int u = 0; u < RUNS; ++u) {
@@ -290,8 +318,38 @@ __device__ __forceinline__ void product_slices(Product p, int work, int tiles_m,
             }
         }
     };
-    if (wave < UNITS) finish(wave, first_out, first_scale);
-    for (int unit = wave + WAVES; unit < UNITS; unit += WAVES) finish(unit, Output(p, min(channel_of(unit, 0), p.N - 1)), scale_of(row_of(unit)));
+    auto output_of = [&](int unit) { return Output(p, min(channel_of(unit, 0), p.N - 1)); };
+    if constexpr (PARTS) {
+        const int parts = sum_parts.parts;
+        if (parts > 1) {
+            Acc* const tile = (Acc*)sum_parts.sums + (int64_t)work * parts * (BM * BN / 4);  // [part][unit][its share][lane]
+            auto at = [&](int of, int unit, int t) { return tile + of * (BM * BN / 4) + (unit * PART + t) * 64 + lane; };
+            for (int unit = wave; unit < UNITS; unit += WAVES) {
+                const Sum sum = sum_of(unit);
+#pragma unroll
+                for (int t = 0; t < PART; ++t) put_part(at(part, unit, t), sum.of[t]);
+            }
+            fence();
+            __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): the wave's part is there
+            fence();
+            __syncthreads();
+            uint32_t* const before = (uint32_t*)smem;
+            if (tid == 0) *before = __hip_atomic_fetch_add(sum_parts.arrived + work, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            __syncthreads();
+            if (*before != (uint32_t)parts - 1) return;
+            for (int unit = wave; unit < UNITS; unit += WAVES) {
+                Sum sum{};
+#pragma unroll 4
+                for (int of = 0; of < parts; ++of)
+#pragma unroll
+                    for (int t = 0; t < PART; ++t) sum.of[t] += get_part(at(of, unit, t));
+                finish(unit, output_of(unit), 1.f, sum);
+            }
+            return;
+        }
+    }
+    if (wave < UNITS) finish(wave, first_out, first_scale, sum_of(wave));
+    for (int unit = wave + WAVES; unit < UNITS; unit += WAVES) finish(unit, output_of(unit), scale_of(row_of(unit)), sum_of(unit));
 }
 
 template <typename T, typename TO, int FORM, int ROWS, int BM, int BN, int WAVES>
@@ -305,15 +363,17 @@ __global__ __launch_bounds__(64 * WAVES, 2) void product_slices_kernel(Product p
 template <typename T, int ROWS, int BM, int WAVES>
 // Every XCD has its share of the rows' tiles, whose sums are long, and behind them its share of the weights'.
 __global__ __launch_bounds__(64 * WAVES, 2) void product_slices_back_kernel(Product rows, Product weights, int rows_m, int rows_n, int rows_per_xcd,
-                                                                            int weights_m, int weights_n, int weights_per_xcd)
+                                                                            int weights_m, int weights_n, int weights_per_xcd, SumParts row_parts,
+                                                                            SumParts weight_parts)
 {
     const int xcd = (int)(blockIdx.x % 8), at = (int)(blockIdx.x / 8);
     if (at < rows_per_xcd) {
         const int work = xcd * rows_per_xcd + at;
-        if (work < rows_m * rows_n) product_slices<T, T, kBackRows, ROWS, BM, 64, WAVES>(rows, work, rows_m, rows_n);
+        if (work < rows_m * rows_n * row_parts.parts) product_slices<T, T, kBackRows, ROWS, BM, 64, WAVES, true>(rows, work, rows_m, rows_n, row_parts);
     } else {
         const int work = xcd * weights_per_xcd + at - rows_per_xcd;
-        if (work < weights_m * weights_n) product_slices<T, T, kBackWeights, ROWS, 64, 64, WAVES>(weights, work, weights_m, weights_n);
+        if (work < weights_m * weights_n * weight_parts.parts)
+            product_slices<T, T, kBackWeights, ROWS, 64, 64, WAVES, true>(weights, work, weights_m, weights_n, weight_parts);
     }
 }
 
@@ -331,7 +391,7 @@ template <typename T, typename TO, int FORM, int ROWS, int BM, int BN> rtoss_sta
     return check_hip(hipGetLastError(), "product launch");
 }
 
-template <typename T, int ROWS, int BM> rtoss_status launch_back(const Product& rows, const Product& weights, hipStream_t s)
+template <typename T, int ROWS, int BM> rtoss_status launch_back(const Product& rows, const Product& weights, SumParts row_parts, SumParts weight_parts, hipStream_t s)
 {
     constexpr int WAVES = 4, LDS = WAVES * (64 + 64) * kStage;
     static LaunchOnce once;
@@ -341,9 +401,9 @@ template <typename T, int ROWS, int BM> rtoss_status launch_back(const Product& 
     if (rtoss_status st = ensure_dynamic_lds((const void*)kernel, LDS, once, dev.device, "LDS of a product")) return st;
     const auto up = [](int64_t n, int by) { return (int)((n + by - 1) / by); };  // (of no result: none)
     const int rows_m = rows.y ? up(rows.M, BM) : 0, rows_n = up(rows.N, 64), weights_m = weights.y ? 2 * up(weights.M, 64) : 0, weights_n = up(weights.N, 64);
-    const int64_t rows_per_xcd = ((int64_t)rows_m * rows_n + 7) / 8, weights_per_xcd = ((int64_t)weights_m * weights_n + 7) / 8;
+    const int64_t rows_per_xcd = ((int64_t)rows_m * rows_n * row_parts.parts + 7) / 8, weights_per_xcd = ((int64_t)weights_m * weights_n * weight_parts.parts + 7) / 8;
     kernel<<<(unsigned)((rows_per_xcd + weights_per_xcd) * 8), 64 * WAVES, LDS, s>>>(rows, weights, rows_m, rows_n, (int)rows_per_xcd, weights_m, weights_n,
-                                                                                       (int)weights_per_xcd);
+                                                                                       (int)weights_per_xcd, row_parts, weight_parts);
     return check_hip(hipGetLastError(), "product launch");
 }
 
@@ -392,11 +452,12 @@ rtoss_status launch_product_slices(ProductForm form, bool bits8, rtoss_dtype out
 }
 
 namespace {
-template <typename T> rtoss_status launch_back_rows(bool high, const Product& rows, const Product& weights, hipStream_t s)
+template <typename T>
+rtoss_status launch_back_rows(bool high, const Product& rows, const Product& weights, SumParts row_parts, SumParts weight_parts, hipStream_t s)
 {
     const auto tile = [&](auto mode) {
         constexpr int ROWS = decltype(mode)::value;
-        return high ? launch_back<T, ROWS, 64>(rows, weights, s) : launch_back<T, ROWS, 16>(rows, weights, s);
+        return high ? launch_back<T, ROWS, 64>(rows, weights, row_parts, weight_parts, s) : launch_back<T, ROWS, 16>(rows, weights, row_parts, weight_parts, s);
     };
     switch (std::max(product_rows(kBackRows, rows, (int)sizeof(T)), product_rows(kBackWeights, weights, (int)sizeof(T)))) {
     case kWhole: return tile(std::integral_constant<int, kWhole>{});
@@ -406,12 +467,13 @@ template <typename T> rtoss_status launch_back_rows(bool high, const Product& ro
 }
 }  // namespace
 
-rtoss_status launch_product_slices_back(rtoss_dtype dt, bool high, const Product& rows, const Product& weights, hipStream_t s)
+rtoss_status launch_product_slices_back(rtoss_dtype dt, bool high, const Product& rows, const Product& weights, SumParts row_parts, SumParts weight_parts,
+                                        hipStream_t s)
 {
     switch (dt) {
-    case RTOSS_F32: return launch_back_rows<float>(high, rows, weights, s);
-    case RTOSS_F16: return launch_back_rows<f16_t>(high, rows, weights, s);
-    default: return launch_back_rows<bf16_t>(high, rows, weights, s);
+    case RTOSS_F32: return launch_back_rows<float>(high, rows, weights, row_parts, weight_parts, s);
+    case RTOSS_F16: return launch_back_rows<f16_t>(high, rows, weights, row_parts, weight_parts, s);
+    default: return launch_back_rows<bf16_t>(high, rows, weights, row_parts, weight_parts, s);
     }
 }
 

@@ -63,11 +63,17 @@ constexpr int kSliceTiles = 5;
 constexpr int kMaxSliceTiles = 0xffffffff / 512 / 16 * 8;  // (half of what a grid of 512 lanes each may have)
 constexpr struct { int rows, channels, gated; } kSlices[kSliceTiles] = {{16, 16, 16}, {32, 16, 16}, {32, 32, 32}, {64, 32, 16}, {64, 64, 32}};
 rtoss_status launch_product_slices(ProductForm form, bool bits8, rtoss_dtype out, int tile, const Product& p, hipStream_t s);
-// both gradients in one launch, that of the rows in tiles of 64 (high) or 16 rows; one without a result (y) is left out
-rtoss_status launch_product_slices_back(rtoss_dtype dt, bool high, const Product& rows, const Product& weights, hipStream_t s);
-// dg = dh * u * act'(g), du = dh * act(g), both [M][ldd] with zeros from column F on (gated_slopes.hip); ldd: slopes_pitch
+// both gradients in one launch, that of the rows in tiles of 64 (high) or 16 rows, each sum in parts; one without a result (y) is left out
+struct SumParts {
+    int parts;          // workgroups of a tile
+    float* sums;        // of more than one: [tile][part][elements of a tile]
+    uint32_t* arrived;  // [tile], zero
+};
+rtoss_status launch_product_slices_back(rtoss_dtype dt, bool high, const Product& rows, const Product& weights, SumParts row_parts, SumParts weight_parts,
+                                        hipStream_t s);
+// dg = dh * u * act'(g), du = dh * act(g), both [M][ldd] with zeros from column F on (gated_slopes.hip); ldd: slopes_pitch.  Clears `counts` words.
 inline int64_t slopes_pitch(int F, rtoss_dtype dt) { return (int64_t)align_up((size_t)F, 16 / elem_bytes(dt)); }
 rtoss_status launch_gated_slopes(rtoss_dtype dt, rtoss_act act, int64_t M, int F, const void* dh, int64_t ldh, const void* gate, const void* up,
-                                 void* dg, void* du, hipStream_t s);
+                                 void* dg, void* du, uint32_t* counters, int counts, hipStream_t s);
 
 }  // namespace rtoss

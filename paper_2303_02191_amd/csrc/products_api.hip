@@ -3,7 +3,7 @@
 #include <algorithm>
 #include <cmath>
 
-#include "products.h"
+#include "product_tile.h"
 
 namespace rtoss {
 
@@ -75,11 +75,13 @@ rtoss_status gated_desc(const rtoss_gated_desc* desc, rtoss_gated_desc* d)
 }
 
 // The kernel for a product: the one whose estimate is shortest.  All are bound by what a CU can copy in the small, by the matrix instructions
-// in the large, and by whole rounds of workgroups.  Constants as measured (us, 256 CUs; M x K x N):
-//   slices of a x b: the launch 3.4 (64 x 64: 4.6), then 80 KB/us and CU for the rows of both operands.  8-bit 4096 x 4096, rows 1, 64, 128, 256, 512:
-//     5.1, 6.8, 7.8, 10.2, 17.6 with the tile that this takes; 8.5, 9.6, 9.6, 10.2, 17.6 with 64 x 64 for all.
-//   tiles: 6 and 8, then 0.95 and 1.3 a stage of 128 bytes (128 and 256 channels).  Gated bf16 4096 -> 10944, rows 256, 512, 1000, 2048: 62, 117,
-//     183, 360 with 128, 83, 90, 173, 284 with 256 channels; slices of 64 x 64 104, 178, 352, 850.
+// in the large, and by whole rounds of workgroups.  Constants in us, for 256 CUs, fitted to 121 products of the forward pass in all tiles (the choice
+// is 1.6 % longer than the best in the mean); rows of whole 16-byte pieces, of words, of bytes:
+//   slices of a x b: the launch 3, then for each round a little more the larger the tile, and the rows of both operands at 68, 44, 36 KB/us and CU;
+//     fp32 also 1e6 products.  8-bit 4096 x 4096, rows 1, 64, 128, 256, 512: 5.2, 6.7, 7.6, 10.1, 18.0 with the tile that this takes; 8.4, 9.4,
+//     9.4, 10.1, 18.0 with 64 x 64 for all.
+//   tiles: 0 and 2.4, then for each round 6 and 0.86, 1.25, 1.8 a stage of 128 bytes (1.28 with 256 channels).  Gated bf16 4096 -> 10944, rows 256,
+//     512, 1024, 2048: 62, 116, 184, 356 with 128, 84, 89, 176, 285 with 256 channels; slices of 64 x 64 103, 181, 338, 636.
 struct Choice {
     int kernel;   // slices by tile, then the two widths of tiles
     double time;  // us
@@ -91,23 +93,24 @@ Choice choose(ProductForm form, bool bits8, rtoss_dtype out, const Product& p, i
     const double row = (double)p.R * eb * (form == kBackRows ? 2 : 1);
     const auto up = [](int64_t n, int by) { return (double)((n + by - 1) / by); };
     const auto tiles = [&](int rows, int channels) { return up(p.M, rows) * up(p.N, channels) * (form == kBackWeights ? 2 : 1); };
+    const Rows rows = product_rows(form, p, eb);
     Choice best{kSliceTiles - 1, 1e300};
     for (int t = across ? kSliceTiles - 1 : 0; t < kSliceTiles; ++t) {
+        constexpr double kRound[kSliceTiles] = {0.14, 0.18, 0.58, 0.83, 1.5}, kRate[] = {68e3, 44e3, 36e3};
         const int a = kSlices[t].rows, n = gated ? kSlices[t].gated : kSlices[t].channels, b = gated ? 2 * n : n;
         if (tiles(a, n) > kMaxSliceTiles) continue;
         const double count = tiles(a, n) / cus;
         const int together = 160 / (a + b);  // workgroups whose LDS a CU holds
         const double rounds = together >= 2 ? std::max(1.0, count) : std::ceil(count);
-        const double one = std::max((a + b) * row / 80e3, eb == 4 ? a * b * row / eb / 500e3 : 0.0);
-        const double time = (a + b >= 128 ? 4.6 : a + b >= 96 ? 3.8 : 3.4) + rounds * one;
+        const double time = 3 + rounds * (kRound[t] + (a + b) * row / kRate[rows] + (eb == 4 ? a * b * row / eb / 1e6 : 0));
         if (time < best.time) best = Choice{t, time};
     }
     if (product_tiles_ok(bits8, out, p)) {
+        constexpr double kStageTime[] = {0.86, 1.25, 1.8};
         const double stages = std::ceil(row / 128);
-        const int widths = product_pieces_ok(form, p, eb) ? 2 : 1;
-        for (int wide = 0; wide < widths; ++wide) {
+        for (int wide = 0; wide < (rows == kWhole ? 2 : 1); ++wide) {
             const int n = (wide ? 256 : 128) / (gated ? 2 : 1);
-            const double time = (wide ? 8 : 6) + std::ceil(tiles(256, n) / cus) * stages * (wide ? 1.3 : 0.95);
+            const double time = (wide ? 2.4 : 0) + std::ceil(tiles(256, n) / cus) * (6 + stages * (wide ? 1.28 : kStageTime[rows]));
             if (time < best.time) best = Choice{kSliceTiles + wide, time};
         }
     }
@@ -146,35 +149,97 @@ rtoss_status launch_product(ProductForm form, bool bits8, rtoss_dtype out, const
     return RTOSS_OK;
 }
 
-// Both gradients, or one (the other's y is NULL), by the same kernels either way: in one launch of slices where that is shorter than two.
-//   one launch: 3.5 us, then 65 KB/us and CU for the rows of both operands, or the longest sum, four stages at a time (0.6 and 0.75 us for tiles of
-//   16 and 64 rows).  bf16 1024 -> 2752, rows 16, 128, 512, 2048, both gradients with dg and du: 18, 21, 32, 78 us, in two launches 40, 44, 42, 82.
-rtoss_status launch_gradients(rtoss_dtype dt, Product rows, Product weights, hipStream_t s)
+// Both gradients in one launch of slices, that of the rows in tiles of `high` ? 64 : 16 rows.  A sum that would take longer than all the copies is
+// shared by several workgroups, which leave their parts in the workspace.  By the shape and type alone, so that the workspace's size is
+// known without a device: 256 CUs, rows of whole pieces.
+//   bytes   of both operands' rows, for all tiles        steps   of four stages, of the rows' sums and the weights'
+struct Merged {
+    double bytes, row_steps, weight_steps;
+    int64_t row_tiles, weight_tiles;
+    int row_parts, weight_parts;
+    size_t counters() const { return ((row_parts > 1 ? row_tiles : 0) + (weight_parts > 1 ? weight_tiles : 0)) * 4; }
+    size_t row_bytes(bool high) const { return row_parts > 1 ? (size_t)row_tiles * row_parts * (high ? 64 : 16) * 64 * 4 : 0; }
+    size_t weight_bytes() const { return weight_parts > 1 ? (size_t)weight_tiles * weight_parts * 64 * 64 * 4 : 0; }
+    size_t scratch(bool high) const { return align_up(counters(), 256) + row_bytes(high) + weight_bytes(); }
+};
+// us for four stages of tiles of 16 and 64 rows, bytes/us and CU; rows of whole 16-byte pieces, of words, of bytes
+struct MergedSpeed {
+    double low, high, rate;
+};
+const MergedSpeed& merged_speed(rtoss_dtype dt, Rows rows)
+{
+    static const MergedSpeed speeds[2][3] = {{{0.6, 0.75, 89e3}, {0.85, 1.2, 61e3}, {1.25, 1.6, 44e3}}, {{0.78, 1.5, 45e3}, {1.07, 2.6, 38e3}, {}}};  // 16 bits, fp32
+    return speeds[dt == RTOSS_F32][rows];
+}
+Merged merged(rtoss_dtype dt, int64_t M, int K, int F, bool high)
+{
+    const int eb = elem_bytes(dt);
+    const auto up = [](int64_t n, int64_t by) { return (n + by - 1) / by; };
+    Merged g;
+    g.row_tiles = up(M, high ? 64 : 16) * up(K, 64);
+    g.weight_tiles = 2 * up(F, 64) * up(K, 64);
+    g.bytes = (double)g.row_tiles * ((high ? 64 : 16) + 64) * 2 * F * eb + (double)g.weight_tiles * 128 * M * eb;
+    g.row_steps = (double)up(2 * up((int64_t)F * eb, 128), 4);
+    g.weight_steps = (double)up(M * eb, 512);
+    const MergedSpeed& speed = merged_speed(dt, kWhole);
+    // (joining takes 2.5 us, about as long as a part of 3 us is worth)
+    const double copies = std::max(g.bytes / (speed.rate * 256), 5.0);
+    const auto parts = [&](double steps, double step, int64_t tiles) {
+        const double time = steps * step;
+        return time < copies + 2.5 || tiles == 0 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>((int64_t)std::ceil(time / copies), 1024 / tiles));
+    };
+    g.row_parts = parts(g.row_steps, high ? speed.high : speed.low, g.row_tiles);
+    g.weight_parts = parts(g.weight_steps, speed.high, g.weight_tiles);
+    return g;
+}
+
+// How the gradients are computed, of one (the other's y is NULL) by the same kernels as of both: in one launch of slices where that is shorter
+// than two.  One launch: 3.5 us, then the copies, or the longest sum.
+//   bf16 1024 -> 2752, rows 16, 128, 512, 2048, both gradients with dg and du: 19, 21, 32, 78 us, in two launches 40, 44, 42, 83.
+struct GradientPlan {
+    bool one, high;
+    Merged merged;
+};
+rtoss_status plan_gradients(rtoss_dtype dt, const Product& rows, const Product& weights, GradientPlan* plan)
 {
     DeviceInfo dev;
     RTOSS_TRY(current_device(&dev));
     const int eb = elem_bytes(dt);
-    const auto up = [](int64_t n, int by) { return (double)((n + by - 1) / by); };
     double two = choose(kBackWeights, false, dt, weights, dev.cus).time;
     if (rows.M > 0) two += choose(kBackRows, false, dt, rows, dev.cus).time;
-    const double weight_tiles = 2 * up(weights.M, 64) * up(weights.N, 64), stages = std::ceil(rows.R * eb / 128.0) * 2;
-    bool high = false;
-    double one = 1e300;
-    for (int t = 0; t < 2; ++t) {
-        const int a = t ? 64 : 16;
-        const double row_tiles = up(rows.M, a) * up(rows.N, 64);
-        if (row_tiles + weight_tiles > kMaxSliceTiles) continue;
-        const double bytes = row_tiles * (a + 64) * 2.0 * rows.R * eb + weight_tiles * 128.0 * weights.R * eb;
-        const double time = 3.5 + std::max(std::ceil(stages / 4) * (t ? 0.75 : 0.6), bytes / (65e3 * dev.cus));
-        if (time < one) one = time, high = t;
+    const MergedSpeed& speed = merged_speed(dt, std::max(product_rows(kBackRows, rows, eb), product_rows(kBackWeights, weights, eb)));
+    double best = 1e300;
+    for (bool high : {false, true}) {
+        const Merged g = merged(dt, rows.M, rows.N, weights.M, high);
+        if (g.row_tiles + g.weight_tiles > kMaxSliceTiles) continue;
+        const double longest = std::max(g.row_steps / g.row_parts * (high ? speed.high : speed.low), g.weight_steps / g.weight_parts * speed.high);
+        const double time = 3.5 + (g.row_parts > 1 || g.weight_parts > 1 ? 2.5 : 0) + std::max(longest, g.bytes / (speed.rate * dev.cus));
+        if (time < best) best = time, *plan = GradientPlan{true, high, g};
     }
-    if (one < two) return launch_product_slices_back(dt, high, rows, weights, s);
+    if (best >= two) *plan = GradientPlan{};
+    return RTOSS_OK;
+}
+
+rtoss_status launch_gradients(rtoss_dtype dt, const GradientPlan& plan, const Product& rows, const Product& weights, void* scratch, hipStream_t s)
+{
+    if (plan.one) {
+        const Merged& g = plan.merged;
+        uint32_t* const arrived = (uint32_t*)scratch;
+        float* const sums = (float*)((char*)scratch + align_up(g.counters(), 256));
+        const SumParts row_parts{g.row_parts, sums, arrived};
+        const SumParts weight_parts{g.weight_parts, (float*)((char*)sums + g.row_bytes(plan.high)), arrived + (g.row_parts > 1 ? g.row_tiles : 0)};
+        return launch_product_slices_back(dt, plan.high, rows, weights, row_parts, weight_parts, s);
+    }
     if (rows.y) RTOSS_TRY(launch_product(kBackRows, false, dt, rows, s));
     if (weights.y) RTOSS_TRY(launch_product(kBackWeights, false, dt, weights, s));
     return RTOSS_OK;
 }
 
 size_t slopes_bytes(const rtoss_gated_desc& d) { return align_up((size_t)d.M * slopes_pitch(d.F, d.dt) * elem_bytes(d.dt), 256); }
+size_t gradient_scratch(const rtoss_gated_desc& d)
+{
+    return align_up(std::max(merged(d.dt, d.M, d.K, d.F, false).scratch(false), merged(d.dt, d.M, d.K, d.F, true).scratch(true)), 256);
+}
 
 }  // namespace
 
@@ -326,7 +391,7 @@ rtoss_status rtoss_gated_ff_backward_size(const rtoss_gated_desc* desc, size_t* 
     rtoss_gated_desc d;
     RTOSS_TRY(gated_desc(desc, &d));
     if (!workspace_bytes) return fail(RTOSS_EINVAL, "size output pointer is NULL");
-    *workspace_bytes = 2 * slopes_bytes(d);
+    *workspace_bytes = 2 * slopes_bytes(d) + gradient_scratch(d);
     return RTOSS_OK;
 }
 
@@ -352,7 +417,7 @@ rtoss_status rtoss_gated_ff_backward(const rtoss_gated_desc* desc, const void* d
             RTOSS_TRY(check_pointer(w_up_dev, eb, "w_up_dev"));
         }
     }
-    const size_t need = 2 * slopes_bytes(d);
+    const size_t need = 2 * slopes_bytes(d) + gradient_scratch(d);
     if (workspace_bytes < need) return fail(RTOSS_ENOSPACE, "workspace has %zu bytes, %zu needed", workspace_bytes, need);
     if (need && !workspace_dev) return fail(RTOSS_EINVAL, "workspace_dev is NULL");
     if (misaligned(workspace_dev, 256)) return fail(RTOSS_EINVAL, "workspace_dev is not 256-byte aligned");
@@ -369,7 +434,6 @@ rtoss_status rtoss_gated_ff_backward(const rtoss_gated_desc* desc, const void* d
     }
     const hipStream_t s = (hipStream_t)hip_stream;
     void *dg = workspace_dev, *du = (char*)workspace_dev + slopes_bytes(d);
-    if (d.M > 0) RTOSS_TRY(launch_gated_slopes(d.dt, d.act, d.M, d.F, dh_dev, d.h_ld, gate_dev, up_dev, dg, du, s));
     Product p{};
     p.a0 = dg;
     p.a1 = du;
@@ -389,7 +453,13 @@ rtoss_status rtoss_gated_ff_backward(const rtoss_gated_desc* desc, const void* d
     to_weights.R = (int)d.M;
     to_weights.y = dw_gate_dev;
     to_weights.y1 = dw_up_dev;
-    return launch_gradients(d.dt, to_rows, to_weights, s);
+    void* const scratch = (char*)workspace_dev + 2 * slopes_bytes(d);
+    GradientPlan plan;
+    RTOSS_TRY(plan_gradients(d.dt, to_rows, to_weights, &plan));
+    const int counts = plan.one ? (int)(plan.merged.counters() / 4) : 0;
+    if (d.M > 0)
+        RTOSS_TRY(launch_gated_slopes(d.dt, d.act, d.M, d.F, dh_dev, d.h_ld, gate_dev, up_dev, dg, du, (uint32_t*)scratch, counts, s));
+    return launch_gradients(d.dt, plan, to_rows, to_weights, scratch, s);
 }
 
 }  // extern "C"

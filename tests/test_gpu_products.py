@@ -288,6 +288,63 @@ def test_gradients_of_whole_numbers(M, K, F, dt):
             equal(dwu, (du.t() @ x.double()).to(t), "dw_up, pitch %d" % pitch)
 
 
+# sums long enough for several workgroups a tile: of the rows (few rows, many channels), of the weights (many rows), of both
+LONG = [(3, 40, 6000), (20, 70, 3333), (130, 64, 9000), (4100, 33, 20), (9000, 200, 100), (1500, 60, 1600), (1, 16, 10944), (8192, 16, 16)]
+
+
+@pytest.mark.parametrize("dt", list(DT))
+@pytest.mark.parametrize("M,K,F", LONG)
+def test_gradients_of_long_sums(M, K, F, dt):
+    """dg and du are at most 4, sums of up to 2 * 10944 products of at most 8 exact."""
+    g = gen(M + 11 * K + F)
+    t = DT[dt]
+    x, wg, wu = whole(g, (M, K), 2, t), whole(g, (F, K), 2, t), whole(g, (F, K), 2, t)
+    gate, up, dh = (whole(g, (M, F), 2, t) for _ in range(3))
+    dg, du = dh.double() * up.double(), dh.double() * gate.double()
+    want = [(dg @ wg.double() + du @ wu.double()).to(t), (dg.t() @ x.double()).to(t), (du.t() @ x.double()).to(t)]
+    for rep in range(3):
+        for a, b, what in zip(pl.gated_ff_backward(dh, x, wg, wu, gate, up, act=0), want, ("dx", "dw_gate", "dw_up")):
+            equal(a, b, what)
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("M,K,F", [(20, 70, 3333), (8192, 64, 40), (1500, 60, 1600)])
+def test_long_sums_have_one_order(M, K, F, dt):
+    """The same bits in every call, on two streams at once, of one gradient alone, and from a replayed graph."""
+    g = gen(M * K + F)
+    t = DT[dt]
+    x, wg, wu = normal(g, (M, K)).to(t), normal(g, (F, K), K ** -0.5).to(t), normal(g, (F, K), K ** -0.5).to(t)
+    gate, up, dh = (normal(g, (M, F)).to(t) for _ in range(3))
+
+    def run():
+        return pl.gated_ff_backward(dh, x, wg, wu, gate, up)
+
+    want = run()
+    equal(pl.gated_ff_backward(dh, x, wg, wu, gate, up, weights=False)[0], want[0])
+    for a, b in zip(pl.gated_ff_backward(dh, x, wg, wu, gate, up, rows=False)[1:], want[1:]):
+        equal(a, b)
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream(), torch.cuda.Stream()], []
+    for _ in range(5):
+        for s in streams:
+            with torch.cuda.stream(s):
+                got.append(run())
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = run()
+    for rep in range(4):
+        run()
+        for v in out:
+            v.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        got.append([v.clone() for v in out])
+    for i, some in enumerate(got):
+        for a, b in zip(some, want):
+            equal(a, b, "call %d" % i)
+
+
 def _silu_slope(v):
     s = torch.sigmoid(v)
     return s * (1 + v * (1 - s))
