@@ -34,11 +34,10 @@ namespace rtoss {
 
 namespace {
 
-constexpr int kTileM = 256;
 constexpr int kRegion = 128 * kStage;       // 128 rows of an operand
 constexpr int kGroupM = 4;                  // row tiles that neighbouring workgroups share
 
-template <typename T, typename TO, int FORM, int TILE_N, int ROWS>
+template <typename T, typename TO, int FORM, int TILE_M, int TILE_N, int ROWS>
 __global__ __launch_bounds__(512, 2) void product_tiles_kernel(Product p, int tiles_m, int tiles_n, int tiles, int per_xcd)
 {
     typedef typename AccOf<T>::type Acc;
@@ -47,8 +46,9 @@ __global__ __launch_bounds__(512, 2) void product_tiles_kernel(Product p, int ti
     constexpr int EB = (int)sizeof(T), STAGE = kStage / EB;  // rows of the sum in a stage
     constexpr int COLS = GATED ? TILE_N / 2 : TILE_N;        // channels of a tile
     constexpr int WN = TILE_N / 64, WM = 8 / WN, MT = 8 / WM;  // waves across channels and rows; row tiles of a wave in half of the rows
-    constexpr int B_REGIONS = TILE_N / 128, kBuffer = (2 + B_REGIONS) * kRegion;  // halves of A, then B
-    extern __shared__ __attribute__((aligned(16))) char smem[];  // two buffers
+    constexpr int HALVES = TILE_M / 128, B_REGIONS = TILE_N / 128, kBuffer = (HALVES + B_REGIONS) * kRegion;  // halves of A, then B
+    constexpr int BUFFERS = HALVES == 2 ? 2 : 4;
+    extern __shared__ __attribute__((aligned(16))) char smem[];  // stage s in buffer s % BUFFERS
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave / WN, wn = wave % WN;
@@ -68,7 +68,7 @@ __global__ __launch_bounds__(512, 2) void product_tiles_kernel(Product p, int ti
             p.y = p.y1;
         }
     }
-    const int64_t m0 = (int64_t)tile_m * kTileM;
+    const int64_t m0 = (int64_t)tile_m * TILE_M;
     const int n0 = at / high * COLS;
 
     const int64_t lda = p.lda * EB, ldb = p.ldb * EB, row = (int64_t)p.R * EB;
@@ -90,7 +90,7 @@ __global__ __launch_bounds__(512, 2) void product_tiles_kernel(Product p, int ti
     // A lane's channel is such that its results are neighbouring channels ----
     const int sub = lane >> 3, piece = (lane & 7) ^ sub;
     constexpr int PIECES = Across<T, 128>::kPieces, COPY_ROWS = Across<T, 128>::kCopyRows;
-    struct Place {  // of a lane's pieces: 0 .. 3 of A's halves, 4 and 5 of B
+    struct Place {  // of a lane's pieces: two of each half of A, then two of B
         char* smem;
         int wave, lane;
         bool late;
@@ -103,7 +103,7 @@ __global__ __launch_bounds__(512, 2) void product_tiles_kernel(Product p, int ti
             else if constexpr (B_REGIONS == 2) return (tile >> 1) * 64 + 16 * (r >> 2) + 4 * (tile & 1) + (r & 3);
             else return (tile >> 2) * 64 + 16 * (r >> 2) + 4 * (tile & 3) + (r & 3);
         }
-        static __device__ __forceinline__ bool of_a(int i) { return i < 4; }
+        static __device__ __forceinline__ bool of_a(int i) { return i < 2 * HALVES; }
         __device__ __forceinline__ int row(int i, int lane) const
         {
             if (of_a(i) ? A_ACROSS : B_ACROSS) return (wave * 2 + i % 2) * COPY_ROWS + lane / PIECES;
@@ -115,7 +115,7 @@ __global__ __launch_bounds__(512, 2) void product_tiles_kernel(Product p, int ti
         __device__ __forceinline__ char* to(int i, int stage) const
         {
             const int spread = (of_a(i) ? A_ACROSS : B_ACROSS) ? Across<T, 128>::spread((wave * 2 + i % 2) * COPY_ROWS + lane / PIECES) : lane >> 3;
-            return smem + (stage & 1) * kBuffer + i / 2 * kRegion + wave * 2048 + i % 2 * 1024 + (lane ^ spread) * 16;
+            return smem + stage % BUFFERS * kBuffer + i / 2 * kRegion + wave * 2048 + i % 2 * 1024 + (lane ^ spread) * 16;
         }
     };
     uint32_t va[2], vb[2];
@@ -131,38 +131,38 @@ __global__ __launch_bounds__(512, 2) void product_tiles_kernel(Product p, int ti
             vb[i] = (uint32_t)Place::channel(rho) * (uint32_t)ldb + piece * 16;
         }
     }
-    // kind: 0, 1 halves of A; 2, 3 regions of B.  Gated with one region: w_gate's rows, then w_up's, which are the upper waves' to copy
+    // kind: the halves of A, then the regions of B.  Gated with one region: w_gate's rows, then w_up's, which are the upper waves' to copy
     auto issue = [&](int stage, int kind) {
-        char* to = smem + (stage & 1) * kBuffer + kind * kRegion + wave * 2048;
+        char* to = smem + stage % BUFFERS * kBuffer + kind * kRegion + wave * 2048;
         int st = min(stage, S - 1);
         const bool second = FORM == kBackRows && st >= S1;  // uniform: the second pair of operands
         if (second) st -= S1;
         __amdgpu_buffer_rsrc_t from;
-        if (kind < 2) {
+        if (kind < HALVES) {
             const int64_t k = A_ACROSS ? (int64_t)st * STAGE * lda : (int64_t)st * kStage;
             from = (second ? a1 : a0).at(k + kind * (A_ACROSS ? 128 * EB : 128 * lda));
         } else {
             const int64_t k = B_ACROSS ? (int64_t)st * STAGE * ldb : (int64_t)st * kStage;
-            const bool other = GATED ? (B_REGIONS == 2 ? kind == 3 : late) : second;
-            from = (other ? b1 : b0).at(k + (kind - 2) * (GATED ? 0 : B_ACROSS ? 128 * EB : 8 * ldb));
+            const bool other = GATED ? (B_REGIONS == 2 ? kind == HALVES + 1 : late) : second;
+            from = (other ? b1 : b0).at(k + (kind - HALVES) * (GATED ? 0 : B_ACROSS ? 128 * EB : 8 * ldb));
         }
 #pragma unroll
         for (int i = 0; i < 2; ++i)
         {
-            const uint32_t offset = kind < 2 ? va[i] : vb[i];
+            const uint32_t offset = kind < HALVES ? va[i] : vb[i];
             if constexpr (B_ACROSS) copy16_bounded(from, offset, __builtin_amdgcn_readfirstlane(lds_offset(to + i * 1024)));
             else __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)(to + i * 1024), 16, offset, 0, 0, 0);
         }
     };
 
-    // ---- rows that are no whole pieces: through registers, a stage's six pieces of a lane at once ----
+    // ---- rows that are no whole pieces: through registers, a stage's pieces of a lane at once ----
     static_assert(ROWS == kWhole || B_REGIONS == 1, "the second region's channels");
     constexpr int PA = A_ACROSS ? PIECES : 8, PB = B_ACROSS ? PIECES : 8;
     const Place place{smem, wave, lane, late};
-    StageInRegisters<T, FORM, ROWS == kWhole ? kWords : ROWS, 6, 4, PA, PB, Place> in_registers(p, place, m0, n0, S1, lane);
-    Acc acc[2 * MT][4];
+    StageInRegisters<T, FORM, ROWS == kWhole ? kWords : ROWS, 2 * HALVES + 2, 2 * HALVES, PA, PB, Place> in_registers(p, place, m0, n0, S1, lane);
+    Acc acc[HALVES * MT][4];
 #pragma unroll
-    for (int i = 0; i < 8 * MT; ++i) acc[i >> 2][i & 3] = Acc{0, 0, 0, 0};
+    for (int i = 0; i < HALVES * MT * 4; ++i) acc[i >> 2][i & 3] = Acc{0, 0, 0, 0};
     u32x4 af[MT][2], bf[4][2];  // [tile][step]
     const int at0 = c * kStage + ((q ^ (c & 7)) * 16);  // by rows: place of piece q of row c; of piece 4 + q: the same with bit 6 flipped
     int at_a[MT], at_b[4 / B_REGIONS];
@@ -188,7 +188,7 @@ __global__ __launch_bounds__(512, 2) void product_tiles_kernel(Product p, int ti
     auto read_b = [&](int buf) {
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
-            const char* base = smem + buf * kBuffer + (2 + t / PLACES) * kRegion;
+            const char* base = smem + buf * kBuffer + (HALVES + t / PLACES) * kRegion;
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
                 if constexpr (B_ACROSS) bf[t][s] = Across<T, 128>::read(base + at_b[t % PLACES] + s * (kRegion / 2));
@@ -214,18 +214,19 @@ __global__ __launch_bounds__(512, 2) void product_tiles_kernel(Product p, int ti
         __builtin_amdgcn_sched_barrier(0);
         fence();
     };
-    constexpr int BEHIND = 4 + 2 * B_REGIONS;
-    auto landed = [&] {  // vmcnt: the copies of all but the newest regions, two of A and those of B; lgkmcnt(0): operands
+    constexpr int BEHIND = HALVES == 2 ? 4 + 2 * B_REGIONS : 8;
+    auto landed = [&] {  // vmcnt: the copies of all but the newest regions, two of A and those of B (one half: two stages'); lgkmcnt(0): operands
         fence();
         __builtin_amdgcn_s_waitcnt(ROWS == kWhole ? 0x0070 | BEHIND : 0xc07f);
     };
     auto issue_first = [&](int stage) {
 #pragma unroll
-        for (int r = 0; r < B_REGIONS; ++r) issue(stage, 2 + r);
+        for (int r = 0; r < B_REGIONS; ++r) issue(stage, HALVES + r);
         issue(stage, 0);
     };
     if constexpr (ROWS == kWhole) {
-        issue_first(0), issue(0, 1), issue_first(1);
+        if constexpr (HALVES == 2) issue_first(0), issue(0, 1), issue_first(1);
+        else issue_first(0), issue_first(1), issue_first(2);
     } else {
         if (S > 0) {  // (a sum of nothing has no memory behind its operands)
             in_registers.load(0);
@@ -238,9 +239,20 @@ __global__ __launch_bounds__(512, 2) void product_tiles_kernel(Product p, int ti
     if (late) meet();  // half of the waves are a part behind the others
     for (int s = 0; s < S; ++s) {
         const bool part = rest < STAGE && (s == S - 1 || (FORM == kBackRows && s == S1 - 1));  // uniform: the sum ends in this stage
-        read_b(s & 1);
-        read_a(s & 1, 0);
-        if constexpr (ROWS == kWhole) issue(s + 1, 1);
+        const int buf = s % BUFFERS;
+        // (the buffer that is filled has been read: both groups of waves are past a barrier behind its last part)
+        auto fill = [&] {
+            if constexpr (ROWS == kWhole) {
+                issue_first(s + (HALVES == 2 ? 2 : 3));
+            } else if (s + 1 < S) {
+                in_registers.store(s + 1);
+                if (s + 2 < S) in_registers.load(s + 2);
+            }
+        };
+        read_b(buf);
+        read_a(buf, 0);
+        if constexpr (HALVES == 1) fill();
+        else if constexpr (ROWS == kWhole) issue(s + 1, 1);
         landed();
         meet();
         if (ROWS == kWhole && part) {
@@ -251,21 +263,17 @@ __global__ __launch_bounds__(512, 2) void product_tiles_kernel(Product p, int ti
         }
         multiply(0);
         meet();
+        if constexpr (HALVES == 1) continue;
 
-        read_a(s & 1, 1);
-        if constexpr (ROWS == kWhole) {
-            issue_first(s + 2);
-        } else if (s + 1 < S) {  // (the other buffer has been read: both groups of waves are past a barrier behind its last part)
-            in_registers.store(s + 1);
-            if (s + 2 < S) in_registers.load(s + 2);
-        }
+        read_a(buf, 1);
+        fill();
         landed();
         meet();
         if (ROWS == kWhole && part) {
 #pragma unroll
             for (int i = 0; i < 2 * MT; ++i) clear_past(af[i >> 1][i & 1], i & 1);
         }
-        multiply(1);
+        multiply(HALVES - 1);
         meet();
     }
     if (!late) meet();
@@ -281,7 +289,7 @@ __global__ __launch_bounds__(512, 2) void product_tiles_kernel(Product p, int ti
         if (n >= p.N) continue;
         const RunOutput<FORM, T, TO, RUN> out(p, n);
 #pragma unroll
-        for (int i = 0; i < 2 * MT; ++i) {
+        for (int i = 0; i < HALVES * MT; ++i) {
             const int64_t m = m0 + i / MT * 128 + (wm * MT + i % MT) * 16 + c;
             if (m >= p.M) continue;
             Acc first[RUN / 4], second[RUN / 4];
@@ -295,15 +303,15 @@ __global__ __launch_bounds__(512, 2) void product_tiles_kernel(Product p, int ti
     }
 }
 
-template <typename T, typename TO, int FORM, int TILE_N, int ROWS> rtoss_status launch(const Product& p, hipStream_t s)
+template <typename T, typename TO, int FORM, int TILE_M, int TILE_N, int ROWS> rtoss_status launch(const Product& p, hipStream_t s)
 {
-    constexpr int COLS = FORM == kGated ? TILE_N / 2 : TILE_N, LDS = 2 * (2 + TILE_N / 128) * kRegion;
+    constexpr int COLS = FORM == kGated ? TILE_N / 2 : TILE_N, LDS = TILE_M == 256 ? 2 * (2 + TILE_N / 128) * kRegion : 4 * 2 * kRegion;
     static LaunchOnce once;
     DeviceInfo dev;
     if (rtoss_status st = current_device(&dev)) return st;
-    const auto kernel = product_tiles_kernel<T, TO, FORM, TILE_N, ROWS>;
+    const auto kernel = product_tiles_kernel<T, TO, FORM, TILE_M, TILE_N, ROWS>;
     if (rtoss_status st = ensure_dynamic_lds((const void*)kernel, LDS, once, dev.device, "LDS of a product")) return st;
-    const int tiles_m = (int)(((int64_t)p.M + kTileM - 1) / kTileM) * (FORM == kBackWeights ? 2 : 1), tiles_n = (p.N + COLS - 1) / COLS;
+    const int tiles_m = (int)(((int64_t)p.M + TILE_M - 1) / TILE_M) * (FORM == kBackWeights ? 2 : 1), tiles_n = (p.N + COLS - 1) / COLS;
     const int64_t tiles = (int64_t)tiles_m * tiles_n;
     const int64_t per_xcd = (tiles + 7) / 8;
     kernel<<<(unsigned)(per_xcd * 8), 512, LDS, s>>>(p, tiles_m, tiles_n, (int)tiles, (int)per_xcd);
@@ -326,35 +334,41 @@ bool product_pieces_ok(ProductForm form, const Product& p, int eb)
 
 bool product_tiles_ok(bool bits8, rtoss_dtype out, const Product& p)
 {
-    return (bits8 || out != RTOSS_F32) && p.R > 0 && (((int64_t)p.M + kTileM - 1) / kTileM) * (((int64_t)p.N + 63) / 64) <= kMaxGridGroups / 4;
+    return (bits8 || out != RTOSS_F32) && p.R > 0 && (((int64_t)p.M + 127) / 128) * (((int64_t)p.N + 63) / 64) <= kMaxGridGroups / 4;
 }
 
 namespace {
-template <typename T, typename TO, int FORM> rtoss_status launch_width(bool wide, const Product& p, hipStream_t s)
+template <typename T, typename TO, int FORM, int ROWS> rtoss_status launch_rows(int tile, const Product& p, hipStream_t s)
+{
+    if constexpr (ROWS == kWhole)
+        if (tile == 2) return launch<T, TO, FORM, 256, 256, ROWS>(p, s);
+    return tile == 0 ? launch<T, TO, FORM, 128, 128, ROWS>(p, s) : launch<T, TO, FORM, 256, 128, ROWS>(p, s);
+}
+template <typename T, typename TO, int FORM> rtoss_status launch_tile(int tile, const Product& p, hipStream_t s)
 {
     switch (product_rows((ProductForm)FORM, p, (int)sizeof(T))) {
-    case kWhole: return wide ? launch<T, TO, FORM, 256, kWhole>(p, s) : launch<T, TO, FORM, 128, kWhole>(p, s);
-    case kWords: return launch<T, TO, FORM, 128, kWords>(p, s);
-    default: return launch<T, TO, FORM, 128, sizeof(T) == 4 ? kWords : kBytes>(p, s);  // (elements of four bytes are words)
+    case kWhole: return launch_rows<T, TO, FORM, kWhole>(tile, p, s);
+    case kWords: return launch_rows<T, TO, FORM, kWords>(tile, p, s);
+    default: return launch_rows<T, TO, FORM, sizeof(T) == 4 ? kWords : kBytes>(tile, p, s);  // (elements of four bytes are words)
     }
 }
-template <typename T> rtoss_status launch_form(ProductForm form, bool wide, const Product& p, hipStream_t s)
+template <typename T> rtoss_status launch_form(ProductForm form, int tile, const Product& p, hipStream_t s)
 {
-    return form == kGated ? launch_width<T, T, kGated>(wide, p, s) : form == kBackRows ? launch_width<T, T, kBackRows>(wide, p, s)
-                                                                                        : launch_width<T, T, kBackWeights>(wide, p, s);
+    return form == kGated ? launch_tile<T, T, kGated>(tile, p, s) : form == kBackRows ? launch_tile<T, T, kBackRows>(tile, p, s)
+                                                                                        : launch_tile<T, T, kBackWeights>(tile, p, s);
 }
-template <typename TO> rtoss_status launch_bits8(ProductForm form, bool wide, const Product& p, hipStream_t s)
+template <typename TO> rtoss_status launch_bits8(ProductForm form, int tile, const Product& p, hipStream_t s)
 {
-    return form == kScaled ? launch_width<int8_t, TO, kScaled>(wide, p, s) : launch_width<int8_t, TO, kGated>(wide, p, s);
+    return form == kScaled ? launch_tile<int8_t, TO, kScaled>(tile, p, s) : launch_tile<int8_t, TO, kGated>(tile, p, s);
 }
 }  // namespace
 
-rtoss_status launch_product_tiles(ProductForm form, bool bits8, rtoss_dtype out, bool wide, const Product& p, hipStream_t s)
+rtoss_status launch_product_tiles(ProductForm form, bool bits8, rtoss_dtype out, int tile, const Product& p, hipStream_t s)
 {
     switch (out) {
-    case RTOSS_F32: return launch_bits8<float>(form, wide, p, s);  // (8-bit operands: product_tiles_ok)
-    case RTOSS_F16: return bits8 ? launch_bits8<f16_t>(form, wide, p, s) : launch_form<f16_t>(form, wide, p, s);
-    default: return bits8 ? launch_bits8<bf16_t>(form, wide, p, s) : launch_form<bf16_t>(form, wide, p, s);
+    case RTOSS_F32: return launch_bits8<float>(form, tile, p, s);  // (8-bit operands: product_tiles_ok)
+    case RTOSS_F16: return bits8 ? launch_bits8<f16_t>(form, tile, p, s) : launch_form<f16_t>(form, tile, p, s);
+    default: return bits8 ? launch_bits8<bf16_t>(form, tile, p, s) : launch_form<bf16_t>(form, tile, p, s);
     }
 }
 

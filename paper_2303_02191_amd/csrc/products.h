@@ -54,9 +54,10 @@ rtoss_status launch_quantize_rows(const void* x, rtoss_dtype dt, int64_t M, int 
                                   hipStream_t s);
 // Every form: kScaled and kGated on 8-bit operands, kGated and the gradients on operands of the result's type.
 bool product_pieces_ok(ProductForm form, const Product& p, int eb);  // rows are whole 16-byte pieces (product_tiles.hip)
-// ... in tiles of 256 rows and 256 (wide) or 128 channels, of 8- and 16-bit operands (product_tiles.hip)
+// ... in tiles of 128 or 256 rows and 128 or 256 channels (kTiles), of 8- and 16-bit operands (product_tiles.hip); the last for whole pieces only
 bool product_tiles_ok(bool bits8, rtoss_dtype out, const Product& p);
-rtoss_status launch_product_tiles(ProductForm form, bool bits8, rtoss_dtype out, bool wide, const Product& p, hipStream_t s);
+constexpr struct { int rows, channels; } kTiles[3] = {{128, 128}, {256, 128}, {256, 256}};
+rtoss_status launch_product_tiles(ProductForm form, bool bits8, rtoss_dtype out, int tile, const Product& p, hipStream_t s);
 // ... of few tiles, and fp32: the sum split over the waves of a workgroup (product_slices.hip).  The tile, rows x channels of a matrix: kSlices;
 // gradients take the last.
 constexpr int kSliceTiles = 5;

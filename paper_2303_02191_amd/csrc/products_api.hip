@@ -75,15 +75,16 @@ rtoss_status gated_desc(const rtoss_gated_desc* desc, rtoss_gated_desc* d)
 }
 
 // The kernel for a product: the one whose estimate is shortest.  All are bound by what a CU can copy in the small, by the matrix instructions
-// in the large, and by whole rounds of workgroups.  Constants in us, for 256 CUs, fitted to 121 products of the forward pass in all tiles (the choice
-// is 1.6 % longer than the best in the mean); rows of whole 16-byte pieces, of words, of bytes:
-//   slices of a x b: the launch 3, then for each round a little more the larger the tile, and the rows of both operands at 68, 44, 36 KB/us and CU;
-//     fp32 also 1e6 products.  8-bit 4096 x 4096, rows 1, 64, 128, 256, 512: 5.2, 6.7, 7.6, 10.1, 18.0 with the tile that this takes; 8.4, 9.4,
-//     9.4, 10.1, 18.0 with 64 x 64 for all.
-//   tiles: 0 and 2.4, then for each round 6 and 0.86, 1.25, 1.8 a stage of 128 bytes (1.28 with 256 channels).  Gated bf16 4096 -> 10944, rows 256,
-//     512, 1024, 2048: 62, 116, 184, 356 with 128, 84, 89, 176, 285 with 256 channels; slices of 64 x 64 103, 181, 338, 636.
+// in the large, and by whole rounds of workgroups.  Constants in us, for 256 CUs, fitted to 456 products of the forward pass in all tiles (the choice
+// is 1.2 % longer than the best in the mean, 25 % at most); rows of whole 16-byte pieces, of words, of bytes:
+//   slices of a x b: the launch 3.1, then for each round a little more the larger the tile, and the rows of both operands at 72, 41, 37 KB/us and CU
+//     (fp32 also 0.77e6 products), or where the sum is short a workgroup's beginning and end.  8-bit 4096 x 4096, rows 1, 64, 128, 256: 5.2, 6.7,
+//     7.6, 9.9 with the tile that this takes; 8.4, 9.4, 9.4, 9.9 with 64 x 64 for all.
+//   tiles: for each round 6, 6, 7 and 0.85, 1.2, 1.8 a stage of 128 bytes; 0.77 and 0.65 of that with 128 rows, 8.9 and 1.26 with 256 channels.
+//     Gated bf16 4096 -> 10944, rows 128, 256, 512, 1024, 2048: 49, 83, 118, 224, 420 with 128 x 128; 58, 62, 117, 184, 351 with 256 x 128; 80, 83,
+//     88, 176, 287 with 256 x 256; slices of 64 x 64 63, 105, 183, 335, 635.
 struct Choice {
-    int kernel;   // slices by tile, then the two widths of tiles
+    int kernel;   // slices by tile, then tiles
     double time;  // us
 };
 Choice choose(ProductForm form, bool bits8, rtoss_dtype out, const Product& p, int cus)
@@ -96,22 +97,25 @@ Choice choose(ProductForm form, bool bits8, rtoss_dtype out, const Product& p, i
     const Rows rows = product_rows(form, p, eb);
     Choice best{kSliceTiles - 1, 1e300};
     for (int t = across ? kSliceTiles - 1 : 0; t < kSliceTiles; ++t) {
-        constexpr double kRound[kSliceTiles] = {0.14, 0.18, 0.58, 0.83, 1.5}, kRate[] = {68e3, 44e3, 36e3};
+        constexpr double kRound[kSliceTiles] = {0.17, 0.24, 0.57, 0.66, 1.57}, kShort[kSliceTiles] = {0.41, 0.58, 1.02, 1.03, 1.4};
+        constexpr double kRate[] = {72e3, 41e3, 37e3}, kAligned[] = {1, 1.77, 2};
         const int a = kSlices[t].rows, n = gated ? kSlices[t].gated : kSlices[t].channels, b = gated ? 2 * n : n;
         if (tiles(a, n) > kMaxSliceTiles) continue;
         const double count = tiles(a, n) / cus;
         const int together = 160 / (a + b);  // workgroups whose LDS a CU holds
         const double rounds = together >= 2 ? std::max(1.0, count) : std::ceil(count);
-        const double time = 3 + rounds * (kRound[t] + (a + b) * row / kRate[rows] + (eb == 4 ? a * b * row / eb / 1e6 : 0));
+        const double sum = kRound[t] + (a + b) * row / kRate[rows] + (eb == 4 ? a * b * row / eb / 0.77e6 : 0);
+        const double time = 3.1 + rounds * std::max(sum, kShort[t] * kAligned[rows] * (gated ? 1.85 : 1) * (eb == 4 ? 1.24 : 1));
         if (time < best.time) best = Choice{t, time};
     }
     if (product_tiles_ok(bits8, out, p)) {
-        constexpr double kStageTime[] = {0.86, 1.25, 1.8};
+        constexpr double kStageTime[] = {0.85, 1.2, 1.8}, kRoundTime[] = {6, 6, 7};
         const double stages = std::ceil(row / 128);
-        for (int wide = 0; wide < (rows == kWhole ? 2 : 1); ++wide) {
-            const int n = (wide ? 256 : 128) / (gated ? 2 : 1);
-            const double time = (wide ? 2.4 : 0) + std::ceil(tiles(256, n) / cus) * (6 + stages * (wide ? 1.28 : kStageTime[rows]));
-            if (time < best.time) best = Choice{kSliceTiles + wide, time};
+        for (int t = 0; t < (rows == kWhole ? 3 : 2); ++t) {
+            const double rounds = std::ceil(tiles(kTiles[t].rows, kTiles[t].channels / (gated ? 2 : 1)) / cus);
+            const double one = t == 2 ? 8.9 + stages * 1.26 : kRoundTime[rows] * (t ? 1 : 0.77) + stages * kStageTime[rows] * (t ? 1 : 0.65);
+            const double time = rounds * one;
+            if (time < best.time) best = Choice{kSliceTiles + t, time};
         }
     }
     return best;
@@ -120,7 +124,7 @@ Choice choose(ProductForm form, bool bits8, rtoss_dtype out, const Product& p, i
 rtoss_status launch_chosen(int kernel, ProductForm form, bool bits8, rtoss_dtype out, const Product& p, hipStream_t s)
 {
     if (kernel < kSliceTiles) return launch_product_slices(form, bits8, out, kernel, p, s);
-    return launch_product_tiles(form, bits8, out, kernel > kSliceTiles, p, s);
+    return launch_product_tiles(form, bits8, out, kernel - kSliceTiles, p, s);
 }
 
 // A launch has at most kMaxSliceTiles of the largest slices: more rows than that take several.
@@ -162,13 +166,14 @@ struct Merged {
     size_t weight_bytes() const { return weight_parts > 1 ? (size_t)weight_tiles * weight_parts * 64 * 64 * 4 : 0; }
     size_t scratch(bool high) const { return align_up(counters(), 256) + row_bytes(high) + weight_bytes(); }
 };
-// us for four stages of tiles of 16 and 64 rows, bytes/us and CU; rows of whole 16-byte pieces, of words, of bytes
+// us for four stages of tiles of 16 and 64 rows, bytes/us and CU, us for a tile and CU; rows of whole 16-byte pieces, of words, of bytes
 struct MergedSpeed {
-    double low, high, rate;
+    double low, high, rate, low_tile, high_tile;
 };
 const MergedSpeed& merged_speed(rtoss_dtype dt, Rows rows)
 {
-    static const MergedSpeed speeds[2][3] = {{{0.6, 0.75, 89e3}, {0.85, 1.2, 61e3}, {1.25, 1.6, 44e3}}, {{0.78, 1.5, 45e3}, {1.07, 2.6, 38e3}, {}}};  // 16 bits, fp32
+    static const MergedSpeed speeds[2][3] = {{{0.4, 0.55, 95e3, 1.1, 1.6}, {0.9, 1.15, 73e3, 1.0, 2.4}, {1.1, 2.0, 52e3, 2.1, 2.85}},  // 16 bits
+                                             {{0.6, 1.6, 56e3, 1.0, 1.85}, {1.08, 2.6, 56e3, 0.6, 3.0}, {}}};                         // fp32
     return speeds[dt == RTOSS_F32][rows];
 }
 Merged merged(rtoss_dtype dt, int64_t M, int K, int F, bool high)
@@ -181,20 +186,20 @@ Merged merged(rtoss_dtype dt, int64_t M, int K, int F, bool high)
     g.bytes = (double)g.row_tiles * ((high ? 64 : 16) + 64) * 2 * F * eb + (double)g.weight_tiles * 128 * M * eb;
     g.row_steps = (double)up(2 * up((int64_t)F * eb, 128), 4);
     g.weight_steps = (double)up(M * eb, 512);
-    const MergedSpeed& speed = merged_speed(dt, kWhole);
-    // (joining takes 2.5 us, about as long as a part of 3 us is worth)
-    const double copies = std::max(g.bytes / (speed.rate * 256), 5.0);
+    // (joining takes 2.5 us, about as long as a part of 3 us is worth; four stages 0.6 and 0.75, fp32 0.78 and 1.5; 89 and 45 KB/us)
+    const double copies = std::max(g.bytes / ((eb == 4 ? 45e3 : 89e3) * 256), 5.0), high_step = eb == 4 ? 1.5 : 0.75;
     const auto parts = [&](double steps, double step, int64_t tiles) {
         const double time = steps * step;
         return time < copies + 2.5 || tiles == 0 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>((int64_t)std::ceil(time / copies), 1024 / tiles));
     };
-    g.row_parts = parts(g.row_steps, high ? speed.high : speed.low, g.row_tiles);
-    g.weight_parts = parts(g.weight_steps, speed.high, g.weight_tiles);
+    g.row_parts = parts(g.row_steps, high ? high_step : eb == 4 ? 0.78 : 0.6, g.row_tiles);
+    g.weight_parts = parts(g.weight_steps, high_step, g.weight_tiles);
     return g;
 }
 
 // How the gradients are computed, of one (the other's y is NULL) by the same kernels as of both: in one launch of slices where that is shorter
-// than two.  One launch: 3.5 us, then the copies, or the longest sum.
+// than two.  One launch: 4.3 us, then the copies and every tile's beginning and end, or the longest sum, or memory; constants fitted to 87 shapes, of
+// which the choice is 0.9 % longer than the best in the mean.
 //   bf16 1024 -> 2752, rows 16, 128, 512, 2048, both gradients with dg and du: 19, 21, 32, 78 us, in two launches 40, 44, 42, 83.
 struct GradientPlan {
     bool one, high;
@@ -213,7 +218,9 @@ rtoss_status plan_gradients(rtoss_dtype dt, const Product& rows, const Product& 
         const Merged g = merged(dt, rows.M, rows.N, weights.M, high);
         if (g.row_tiles + g.weight_tiles > kMaxSliceTiles) continue;
         const double longest = std::max(g.row_steps / g.row_parts * (high ? speed.high : speed.low), g.weight_steps / g.weight_parts * speed.high);
-        const double time = 3.5 + (g.row_parts > 1 || g.weight_parts > 1 ? 2.5 : 0) + std::max(longest, g.bytes / (speed.rate * dev.cus));
+        const double tiles = (double)(g.row_tiles * g.row_parts) * (high ? speed.high_tile : speed.low_tile) + (double)(g.weight_tiles * g.weight_parts) * speed.high_tile;
+        const double moved = (4.0 * weights.M * rows.N + 2.0 * rows.M * (rows.N + weights.M)) * eb / 5.9e6;
+        const double time = 4.3 + (g.row_parts > 1 || g.weight_parts > 1 ? 1.5 : 0) + std::max({longest, g.bytes / (speed.rate * dev.cus) + tiles / dev.cus, moved});
         if (time < best) best = time, *plan = GradientPlan{true, high, g};
     }
     if (best >= two) *plan = GradientPlan{};
