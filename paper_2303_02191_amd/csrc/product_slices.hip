@@ -34,10 +34,14 @@ __device__ __forceinline__ f32x4 get_part(const f32x4* at)
     return __builtin_bit_cast(f32x4, halves);
 }
 
-// One tile of a product, or a part of its sum: `work` of tiles_m x tiles_n x sum.parts.
-template <typename T, typename TO, int FORM, int ROWS, int BM, int BN, int WAVES, bool PARTS = false>
-__device__ __forceinline__ void product_slices(Product p, int work, int tiles_m, int tiles_n, SumParts sum_parts = {1, nullptr, nullptr})
+// How the waves of a workgroup share the work: a tile, a part of a tile's sum, or a tile each.
+enum Shared { kTile, kPart, kTileEach };
+
+// `work` of tiles_m x tiles_n (x sum_parts.parts); kTileEach: the wave's
+template <typename T, typename TO, int FORM, int ROWS, int BM, int BN, int WAVES, int SHARED>
+__device__ __forceinline__ void product_slices(Product p, int work, int tiles_m, int tiles_n, SumParts sum_parts = {})
 {
+    constexpr bool PARTS = SHARED == kPart, EACH = SHARED == kTileEach;
     typedef typename AccOf<T>::type Acc;
     constexpr bool GATED = FORM == kGated;
     constexpr bool A_ACROSS = FORM == kBackWeights, B_ACROSS = FORM == kBackRows || FORM == kBackWeights;
@@ -72,7 +76,7 @@ __device__ __forceinline__ void product_slices(Product p, int work, int tiles_m,
     const int64_t lda = p.lda * EB, ldb = p.ldb * EB, row = (int64_t)p.R * EB;
     const int S1 = (int)(((int64_t)p.R + STAGE - 1) / STAGE), S = FORM == kBackRows ? 2 * S1 : S1;
     const int rest = p.R - (S1 - 1) * STAGE;  // rows of the sum in the last stage
-    const int begin = PARTS ? (int)((int64_t)S * part / sum_parts.parts) : 0, end = PARTS ? (int)((int64_t)S * (part + 1) / sum_parts.parts) : S;
+    const int begin = (PARTS ? (int)((int64_t)S * part / sum_parts.parts) : 0) + (EACH ? 0 : wave), end = PARTS ? (int)((int64_t)S * (part + 1) / sum_parts.parts) : S;
     auto whole = [](int64_t bytes) { return (bytes + 15) & ~(int64_t)15; };  // (dg and du, whose rows are padded)
     auto rows_from = [&](const void* base, int64_t ld, int64_t first, int64_t rows) {
         return Source{(const char*)base + first * ld, (rows - 1 - first) * ld + whole(row)};
@@ -128,7 +132,7 @@ __device__ __forceinline__ void product_slices(Product p, int work, int tiles_m,
         f.up = GATED ? b1.at(kb) : f.b;
         return f;
     };
-    constexpr int PIECES = A_COPIES + B_COPIES;
+    constexpr int PIECES = A_COPIES + B_COPIES, STEP = EACH ? 1 : WAVES;
     auto copy = [&](const From& f, uint32_t to, auto which) {
         constexpr int I = decltype(which)::value;
         if constexpr (I < A_COPIES) copy16_bounded(f.a, va[I], to + I * 1024);
@@ -158,8 +162,9 @@ __device__ __forceinline__ void product_slices(Product p, int work, int tiles_m,
     };
     typedef RunOutput<FORM, T, TO, RUN> Output;
     auto scale_of = [&](int64_t m) { return Output::kScales && p.sa ? p.sa[min(m, (int64_t)p.M - 1)] : 1.f; };
-    const Output first_out(p, min(channel_of(wave, 0), p.N - 1));  // (across: it holds nothing but the place)
-    const float first_scale = scale_of(row_of(wave));
+    const int first_unit = EACH ? 0 : wave;
+    const Output first_out(p, min(channel_of(first_unit, 0), p.N - 1));  // (across: it holds nothing but the place)
+    const float first_scale = scale_of(row_of(first_unit));
 
     auto read_and_multiply = [&](const char* base, int s, auto&& then) {
         u32x4 af[2][MT], bf[2][NT];
@@ -226,8 +231,8 @@ __device__ __forceinline__ void product_slices(Product p, int work, int tiles_m,
             const From f = source(s);
             static_for<PIECES>([&](auto k) { copy(f, lds0, k); });
         };
-        if (begin + wave < end) issue(begin + wave);
-        for (int s = begin + wave; s < end; s += WAVES) {
+        if (begin < end) issue(begin);
+        for (int s = begin; s < end; s += STEP) {
             fence();
             __builtin_amdgcn_s_waitcnt(0x0f70);  // the stage has landed
             fence();
@@ -235,7 +240,7 @@ __device__ __forceinline__ void product_slices(Product p, int work, int tiles_m,
                 fence();
                 __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): its place is free
                 fence();
-                if (s + WAVES < end) issue(s + WAVES);
+                if (s + STEP < end) issue(s + STEP);
                 __builtin_amdgcn_sched_barrier(0);
             });
         }
@@ -265,39 +270,18 @@ __device__ __forceinline__ void product_slices(Product p, int work, int tiles_m,
         };
         const Place place{own, lane};
         StageInRegisters<T, FORM, ROWS, PIECES, A_COPIES, PA, PB, Place> in_registers(p, place, m0, n0, S1, lane);
-        if (begin + wave < end) in_registers.load(begin + wave);
-        for (int s = begin + wave; s < end; s += WAVES) {
+        if (begin < end) in_registers.load(begin);
+        for (int s = begin; s < end; s += STEP) {
             in_registers.store(s);
-            if (s + WAVES < end) in_registers.load(s + WAVES);
+            if (s + STEP < end) in_registers.load(s + STEP);
             fence();
             read_and_multiply(own, s, [&] {});
             fence();
         }
     }
 
-    // ---- join ----
-    __syncthreads();
-    Acc* const joined = (Acc*)smem;  // [wave][row tile][channel tile][lane]
-    static_assert(MT * NT * 1024 <= BUFFER, "the sums fit the waves' places");
-#pragma unroll
-    for (int i = 0; i < MT; ++i)
-#pragma unroll
-        for (int n = 0; n < NT; ++n) joined[((wave * MT + i) * NT + n) * 64 + lane] = acc[i][n];
-    __syncthreads();
     struct Sum {
         Acc of[PART];
-    };
-    auto sum_of = [&](int unit) {
-        const int share = unit % SHARE;
-        Sum sum;
-#pragma unroll
-        for (int t = 0; t < PART; ++t) {
-            const Acc* from = joined + (unit / SHARE * NT + (GATED ? NT / 2 * t + share : PART * share + t)) * 64 + lane;
-            sum.of[t] = from[0];
-#pragma unroll
-            for (int w = 1; w < WAVES; ++w) sum.of[t] += from[w * MT * NT * 64];
-        }
-        return sum;
     };
     auto finish = [&](int unit, const Output& out, float sa, const Sum& of) {
         const auto& sum = of.of;
@@ -319,6 +303,39 @@ __device__ __forceinline__ void product_slices(Product p, int work, int tiles_m,
         }
     };
     auto output_of = [&](int unit) { return Output(p, min(channel_of(unit, 0), p.N - 1)); };
+    if constexpr (EACH) {
+        static_for<UNITS>([&](auto which) {
+            constexpr int unit = which, share = unit % SHARE;
+            Sum sum;
+#pragma unroll
+            for (int t = 0; t < PART; ++t) sum.of[t] = acc[unit / SHARE][GATED ? NT / 2 * t + share : PART * share + t];
+            if constexpr (unit == 0) finish(unit, first_out, first_scale, sum);
+            else finish(unit, output_of(unit), scale_of(row_of(unit)), sum);
+        });
+        return;
+    }
+
+    // ---- join ----
+    __syncthreads();
+    Acc* const joined = (Acc*)smem;  // [wave][row tile][channel tile][lane]
+    static_assert(MT * NT * 1024 <= BUFFER, "the sums fit the waves' places");
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) joined[((wave * MT + i) * NT + n) * 64 + lane] = acc[i][n];
+    __syncthreads();
+    auto sum_of = [&](int unit) {
+        const int share = unit % SHARE;
+        Sum sum;
+#pragma unroll
+        for (int t = 0; t < PART; ++t) {
+            const Acc* from = joined + (unit / SHARE * NT + (GATED ? NT / 2 * t + share : PART * share + t)) * 64 + lane;
+            sum.of[t] = from[0];
+#pragma unroll
+            for (int w = 1; w < WAVES; ++w) sum.of[t] += from[w * MT * NT * 64];
+        }
+        return sum;
+    };
     if constexpr (PARTS) {
         const int parts = sum_parts.parts;
         if (parts > 1) {
@@ -356,24 +373,28 @@ template <typename T, typename TO, int FORM, int ROWS, int BM, int BN, int WAVES
 __global__ __launch_bounds__(64 * WAVES, 2) void product_slices_kernel(Product p, int tiles_m, int tiles_n, int tiles, int per_xcd)
 {
     const int work = (int)(blockIdx.x % 8) * per_xcd + (int)(blockIdx.x / 8);  // (XCD-contiguous)
-    if (work < tiles) product_slices<T, TO, FORM, ROWS, BM, BN, WAVES>(p, work, tiles_m, tiles_n);
+    if (work < tiles) product_slices<T, TO, FORM, ROWS, BM, BN, WAVES, kTile>(p, work, tiles_m, tiles_n);
 }
 
 // Both gradients in one launch (or one, by the same code): they share nothing but dg and du, and each alone leaves most of the chip without work.
-template <typename T, int ROWS, int BM, int WAVES>
-// Every XCD has its share of the rows' tiles, whose sums are long, and behind them its share of the weights'.
+// Every XCD has its share of the rows' tiles, whose sums are long, and behind them its share of the weights'.  ROWS_EACH, WEIGHTS_EACH: of these
+// every wave has one.
+template <typename T, int ROWS, int BM, int WAVES, bool ROWS_EACH, bool WEIGHTS_EACH>
 __global__ __launch_bounds__(64 * WAVES, 2) void product_slices_back_kernel(Product rows, Product weights, int rows_m, int rows_n, int rows_per_xcd,
                                                                             int weights_m, int weights_n, int weights_per_xcd, SumParts row_parts,
                                                                             SumParts weight_parts)
 {
-    const int xcd = (int)(blockIdx.x % 8), at = (int)(blockIdx.x / 8);
+    const int xcd = (int)(blockIdx.x % 8), at = (int)(blockIdx.x / 8), wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     if (at < rows_per_xcd) {
-        const int work = xcd * rows_per_xcd + at;
-        if (work < rows_m * rows_n * row_parts.parts) product_slices<T, T, kBackRows, ROWS, BM, 64, WAVES, true>(rows, work, rows_m, rows_n, row_parts);
+        int work = xcd * rows_per_xcd + at;
+        if constexpr (ROWS_EACH) work = work * WAVES + wave;
+        if (work < rows_m * rows_n * row_parts.parts)
+            product_slices<T, T, kBackRows, ROWS, BM, 64, WAVES, ROWS_EACH ? kTileEach : kPart>(rows, work, rows_m, rows_n, row_parts);
     } else {
-        const int work = xcd * weights_per_xcd + at - rows_per_xcd;
+        int work = xcd * weights_per_xcd + at - rows_per_xcd;
+        if constexpr (WEIGHTS_EACH) work = work * WAVES + wave;
         if (work < weights_m * weights_n * weight_parts.parts)
-            product_slices<T, T, kBackWeights, ROWS, 64, 64, WAVES, true>(weights, work, weights_m, weights_n, weight_parts);
+            product_slices<T, T, kBackWeights, ROWS, 64, 64, WAVES, WEIGHTS_EACH ? kTileEach : kPart>(weights, work, weights_m, weights_n, weight_parts);
     }
 }
 
@@ -391,17 +412,20 @@ template <typename T, typename TO, int FORM, int ROWS, int BM, int BN> rtoss_sta
     return check_hip(hipGetLastError(), "product launch");
 }
 
-template <typename T, int ROWS, int BM> rtoss_status launch_back(const Product& rows, const Product& weights, SumParts row_parts, SumParts weight_parts, hipStream_t s)
+template <typename T, int ROWS, int BM, bool ROWS_EACH, bool WEIGHTS_EACH>
+rtoss_status launch_back(const Product& rows, const Product& weights, SumParts row_parts, SumParts weight_parts, hipStream_t s)
 {
     constexpr int WAVES = 4, LDS = WAVES * (64 + 64) * kStage;
     static LaunchOnce once;
     DeviceInfo dev;
     if (rtoss_status st = current_device(&dev)) return st;
-    const auto kernel = product_slices_back_kernel<T, ROWS, BM, WAVES>;
+    const auto kernel = product_slices_back_kernel<T, ROWS, BM, WAVES, ROWS_EACH, WEIGHTS_EACH>;
     if (rtoss_status st = ensure_dynamic_lds((const void*)kernel, LDS, once, dev.device, "LDS of a product")) return st;
     const auto up = [](int64_t n, int by) { return (int)((n + by - 1) / by); };  // (of no result: none)
     const int rows_m = rows.y ? up(rows.M, BM) : 0, rows_n = up(rows.N, 64), weights_m = weights.y ? 2 * up(weights.M, 64) : 0, weights_n = up(weights.N, 64);
-    const int64_t rows_per_xcd = ((int64_t)rows_m * rows_n * row_parts.parts + 7) / 8, weights_per_xcd = ((int64_t)weights_m * weights_n * weight_parts.parts + 7) / 8;
+    const auto per_xcd = [](int64_t tiles, bool each) { return ((each ? (tiles + WAVES - 1) / WAVES : tiles) + 7) / 8; };
+    const int64_t rows_per_xcd = per_xcd((int64_t)rows_m * rows_n * row_parts.parts, ROWS_EACH);
+    const int64_t weights_per_xcd = per_xcd((int64_t)weights_m * weights_n * weight_parts.parts, WEIGHTS_EACH);
     kernel<<<(unsigned)((rows_per_xcd + weights_per_xcd) * 8), 64 * WAVES, LDS, s>>>(rows, weights, rows_m, rows_n, (int)rows_per_xcd, weights_m, weights_n,
                                                                                        (int)weights_per_xcd, row_parts, weight_parts);
     return check_hip(hipGetLastError(), "product launch");
@@ -457,7 +481,11 @@ rtoss_status launch_back_rows(bool high, const Product& rows, const Product& wei
 {
     const auto tile = [&](auto mode) {
         constexpr int ROWS = decltype(mode)::value;
-        return high ? launch_back<T, ROWS, 64>(rows, weights, row_parts, weight_parts, s) : launch_back<T, ROWS, 16>(rows, weights, row_parts, weight_parts, s);
+        const bool each = weight_parts.each;
+        const auto go = high ? row_parts.each ? each ? launch_back<T, ROWS, 64, true, true> : launch_back<T, ROWS, 64, true, false>
+                                              : each ? launch_back<T, ROWS, 64, false, true> : launch_back<T, ROWS, 64, false, false>
+                             : each ? launch_back<T, ROWS, 16, false, true> : launch_back<T, ROWS, 16, false, false>;
+        return go(rows, weights, row_parts, weight_parts, s);
     };
     switch (std::max(product_rows(kBackRows, rows, (int)sizeof(T)), product_rows(kBackWeights, weights, (int)sizeof(T)))) {
     case kWhole: return tile(std::integral_constant<int, kWhole>{});

@@ -67,7 +67,8 @@ rtoss_status launch_product_slices(ProductForm form, bool bits8, rtoss_dtype out
 // both gradients in one launch, that of the rows in tiles of 64 (high) or 16 rows, each sum in parts; one without a result (y) is left out
 struct SumParts {
     int parts;          // workgroups of a tile
-    float* sums;        // of more than one: [tile][part][elements of a tile]
+    bool each;          // every wave of a workgroup has a tile of its own (one part; rows: high)
+    float* sums;        // of more parts than one: [tile][part][elements of a tile]
     uint32_t* arrived;  // [tile], zero
 };
 rtoss_status launch_product_slices_back(rtoss_dtype dt, bool high, const Product& rows, const Product& weights, SumParts row_parts, SumParts weight_parts,

@@ -161,12 +161,13 @@ struct Merged {
     double bytes, row_steps, weight_steps;
     int64_t row_tiles, weight_tiles;
     int row_parts, weight_parts;
+    bool rows_each, weights_each;
     size_t counters() const { return ((row_parts > 1 ? row_tiles : 0) + (weight_parts > 1 ? weight_tiles : 0)) * 4; }
     size_t row_bytes(bool high) const { return row_parts > 1 ? (size_t)row_tiles * row_parts * (high ? 64 : 16) * 64 * 4 : 0; }
     size_t weight_bytes() const { return weight_parts > 1 ? (size_t)weight_tiles * weight_parts * 64 * 64 * 4 : 0; }
     size_t scratch(bool high) const { return align_up(counters(), 256) + row_bytes(high) + weight_bytes(); }
 };
-// us for four stages of tiles of 16 and 64 rows, bytes/us and CU, us for a tile and CU; rows of whole 16-byte pieces, of words, of bytes
+// us for four stages of tiles of 16 and 64 rows, bytes/us and CU, us for a tile and CU (half of it where every wave has one); rows of whole 16-byte pieces, of words, of bytes
 struct MergedSpeed {
     double low, high, rate, low_tile, high_tile;
 };
@@ -194,6 +195,10 @@ Merged merged(rtoss_dtype dt, int64_t M, int K, int F, bool high)
     };
     g.row_parts = parts(g.row_steps, high ? high_step : eb == 4 ? 0.78 : 0.6, g.row_tiles);
     g.weight_parts = parts(g.weight_steps, high_step, g.weight_tiles);
+    // Of many tiles with short sums every wave takes one, and nothing is joined: bf16 16 rows 1024 -> 2752 17 -> 14 us, 2 rows 990 -> 7682 62 -> 31; at
+    // 1024 rows (16 stages) 54 either way, of 88 tiles with 512 rows 11 -> 14.
+    g.rows_each = high && g.row_steps <= 2 && g.row_tiles >= 1024;
+    g.weights_each = g.weight_steps <= 2 && g.weight_tiles >= 1024;
     return g;
 }
 
@@ -218,7 +223,8 @@ rtoss_status plan_gradients(rtoss_dtype dt, const Product& rows, const Product& 
         const Merged g = merged(dt, rows.M, rows.N, weights.M, high);
         if (g.row_tiles + g.weight_tiles > kMaxSliceTiles) continue;
         const double longest = std::max(g.row_steps / g.row_parts * (high ? speed.high : speed.low), g.weight_steps / g.weight_parts * speed.high);
-        const double tiles = (double)(g.row_tiles * g.row_parts) * (high ? speed.high_tile : speed.low_tile) + (double)(g.weight_tiles * g.weight_parts) * speed.high_tile;
+        const double tiles = g.row_tiles * g.row_parts * (high ? speed.high_tile : speed.low_tile) * (g.rows_each ? 0.5 : 1) +
+                             g.weight_tiles * g.weight_parts * speed.high_tile * (g.weights_each ? 0.5 : 1);
         const double moved = (4.0 * weights.M * rows.N + 2.0 * rows.M * (rows.N + weights.M)) * eb / 5.9e6;
         const double time = 4.3 + (g.row_parts > 1 || g.weight_parts > 1 ? 1.5 : 0) + std::max({longest, g.bytes / (speed.rate * dev.cus) + tiles / dev.cus, moved});
         if (time < best) best = time, *plan = GradientPlan{true, high, g};
@@ -233,8 +239,8 @@ rtoss_status launch_gradients(rtoss_dtype dt, const GradientPlan& plan, const Pr
         const Merged& g = plan.merged;
         uint32_t* const arrived = (uint32_t*)scratch;
         float* const sums = (float*)((char*)scratch + align_up(g.counters(), 256));
-        const SumParts row_parts{g.row_parts, sums, arrived};
-        const SumParts weight_parts{g.weight_parts, (float*)((char*)sums + g.row_bytes(plan.high)), arrived + (g.row_parts > 1 ? g.row_tiles : 0)};
+        const SumParts row_parts{g.row_parts, g.rows_each, sums, arrived};
+        const SumParts weight_parts{g.weight_parts, g.weights_each, (float*)((char*)sums + g.row_bytes(plan.high)), arrived + (g.row_parts > 1 ? g.row_tiles : 0)};
         return launch_product_slices_back(dt, plan.high, rows, weights, row_parts, weight_parts, s);
     }
     if (rows.y) RTOSS_TRY(launch_product(kBackRows, false, dt, rows, s));
