@@ -161,10 +161,10 @@ __device__ __forceinline__ void product_slices(Product p, int work, int tiles_m,
         return n0 + (B_ACROSS ? (PART * share + u) * 16 + 4 * q : GATED ? 2 * NT * q + 4 * share : 4 * NT * q + 4 * PART * share);
     };
     typedef RunOutput<FORM, T, TO, RUN> Output;
-    auto scale_of = [&](int64_t m) { return Output::kScales && p.sa ? p.sa[min(m, (int64_t)p.M - 1)] : 1.f; };
+    auto read_of = [&](const Output& out, int unit) { return out.row(p, min(row_of(unit), (int64_t)p.M - 1)); };
     const int first_unit = EACH ? 0 : wave;
     const Output first_out(p, min(channel_of(first_unit, 0), p.N - 1));  // (across: it holds nothing but the place)
-    const float first_scale = scale_of(row_of(first_unit));
+    const auto first_read = read_of(first_out, first_unit);
 
     auto read_and_multiply = [&](const char* base, int s, auto&& then) {
         u32x4 af[2][MT], bf[2][NT];
@@ -283,7 +283,7 @@ __device__ __forceinline__ void product_slices(Product p, int work, int tiles_m,
     struct Sum {
         Acc of[PART];
     };
-    auto finish = [&](int unit, const Output& out, float sa, const Sum& of) {
+    auto finish = [&](int unit, const Output& out, const typename Output::Row& read, const Sum& of) {
         const auto& sum = of.of;
         const int64_t m = row_of(unit);
         if (m >= p.M) return;
@@ -293,24 +293,27 @@ __device__ __forceinline__ void product_slices(Product p, int work, int tiles_m,
             if (n >= p.N) continue;
             if constexpr (B_ACROSS) {
                 const Acc one[1] = {sum[u]};
-                Output(p, n).store(p, m, sa, one, one);
+                Output(p, n).store(p, m, read, one, one);
             } else if constexpr (GATED) {
                 const Acc first[1] = {sum[0]}, second[1] = {sum[PART - 1]};
-                out.store(p, m, sa, first, second);
+                out.store(p, m, read, first, second);
             } else {
-                out.store(p, m, sa, sum, sum);
+                out.store(p, m, read, sum, sum);
             }
         }
     };
-    auto output_of = [&](int unit) { return Output(p, min(channel_of(unit, 0), p.N - 1)); };
+    auto finish_next = [&](int unit, const Sum& sum) {
+        const Output out(p, min(channel_of(unit, 0), p.N - 1));
+        finish(unit, out, read_of(out, unit), sum);
+    };
     if constexpr (EACH) {
         static_for<UNITS>([&](auto which) {
             constexpr int unit = which, share = unit % SHARE;
             Sum sum;
 #pragma unroll
             for (int t = 0; t < PART; ++t) sum.of[t] = acc[unit / SHARE][GATED ? NT / 2 * t + share : PART * share + t];
-            if constexpr (unit == 0) finish(unit, first_out, first_scale, sum);
-            else finish(unit, output_of(unit), scale_of(row_of(unit)), sum);
+            if constexpr (unit == 0) finish(unit, first_out, first_read, sum);
+            else finish_next(unit, sum);
         });
         return;
     }
@@ -360,20 +363,21 @@ __device__ __forceinline__ void product_slices(Product p, int work, int tiles_m,
                 for (int of = 0; of < parts; ++of)
 #pragma unroll
                     for (int t = 0; t < PART; ++t) sum.of[t] += get_part(at(of, unit, t));
-                finish(unit, output_of(unit), 1.f, sum);
+                finish_next(unit, sum);
             }
             return;
         }
     }
-    if (wave < UNITS) finish(wave, first_out, first_scale, sum_of(wave));
-    for (int unit = wave + WAVES; unit < UNITS; unit += WAVES) finish(unit, output_of(unit), scale_of(row_of(unit)), sum_of(unit));
+    if (wave < UNITS) finish(wave, first_out, first_read, sum_of(wave));
+    for (int unit = wave + WAVES; unit < UNITS; unit += WAVES) finish_next(unit, sum_of(unit));
 }
 
-template <typename T, typename TO, int FORM, int ROWS, int BM, int BN, int WAVES>
+template <typename T, typename TO, int FORM, int ROWS, int BM, int BN, int WAVES, bool EACH>
 __global__ __launch_bounds__(64 * WAVES, 2) void product_slices_kernel(Product p, int tiles_m, int tiles_n, int tiles, int per_xcd)
 {
-    const int work = (int)(blockIdx.x % 8) * per_xcd + (int)(blockIdx.x / 8);  // (XCD-contiguous)
-    if (work < tiles) product_slices<T, TO, FORM, ROWS, BM, BN, WAVES, kTile>(p, work, tiles_m, tiles_n);
+    int work = (int)(blockIdx.x % 8) * per_xcd + (int)(blockIdx.x / 8);  // (XCD-contiguous)
+    if constexpr (EACH) work = work * WAVES + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    if (work < tiles) product_slices<T, TO, FORM, ROWS, BM, BN, WAVES, EACH ? kTileEach : kTile>(p, work, tiles_m, tiles_n);
 }
 
 // Both gradients in one launch (or one, by the same code): they share nothing but dg and du, and each alone leaves most of the chip without work.
@@ -398,16 +402,16 @@ __global__ __launch_bounds__(64 * WAVES, 2) void product_slices_back_kernel(Prod
     }
 }
 
-template <typename T, typename TO, int FORM, int ROWS, int BM, int BN> rtoss_status launch(const Product& p, hipStream_t s)
+template <typename T, typename TO, int FORM, int ROWS, int BM, int BN, bool EACH = false> rtoss_status launch(const Product& p, hipStream_t s)
 {
     constexpr int WAVES = 8, COLS = FORM == kGated ? BN / 2 : BN, LDS = WAVES * (BM + BN) * kStage;
     static LaunchOnce once;
     DeviceInfo dev;
     if (rtoss_status st = current_device(&dev)) return st;
-    const auto kernel = product_slices_kernel<T, TO, FORM, ROWS, BM, BN, WAVES>;
+    const auto kernel = product_slices_kernel<T, TO, FORM, ROWS, BM, BN, WAVES, EACH>;
     if (rtoss_status st = ensure_dynamic_lds((const void*)kernel, LDS, once, dev.device, "LDS of a product")) return st;
     const int tiles_m = (int)(((int64_t)p.M + BM - 1) / BM) * (FORM == kBackWeights ? 2 : 1), tiles_n = (p.N + COLS - 1) / COLS;
-    const int64_t tiles = (int64_t)tiles_m * tiles_n, per_xcd = (tiles + 7) / 8;
+    const int64_t tiles = (int64_t)tiles_m * tiles_n, per_xcd = ((EACH ? (tiles + WAVES - 1) / WAVES : tiles) + 7) / 8;
     kernel<<<(unsigned)(per_xcd * 8), 64 * WAVES, LDS, s>>>(p, tiles_m, tiles_n, (int)tiles, (int)per_xcd);
     return check_hip(hipGetLastError(), "product launch");
 }
@@ -442,6 +446,8 @@ template <typename T, typename TO, int FORM, int ROWS> rtoss_status launch_tile(
         case 3: return launch<T, TO, FORM, ROWS, 64, 32>(p, s);
         }
     }
+    if constexpr (sizeof(T) == 4 && FORM == kGated)
+        if (tile == kSliceTiles) return launch<T, TO, FORM, ROWS, 64, 64, true>(p, s);
     return launch<T, TO, FORM, ROWS, 64, 64>(p, s);
 }
 

@@ -287,18 +287,25 @@ __global__ __launch_bounds__(512, 2) void product_tiles_kernel(Product p, int ti
         const int column = B_REGIONS == 2 ? (u >> 1) * 128 + wn * 32 + (u & 1) * 16 : wn * 64 + u * 16;
         const int n = n0 + (GATED ? wn * 32 : B_ACROSS ? column : wn * 64) + RUN * q;
         if (n >= p.N) continue;
-        const RunOutput<FORM, T, TO, RUN> out(p, n);
+        typedef RunOutput<FORM, T, TO, RUN> Output;
+        const Output out(p, n);
+        auto row_of = [&](int i) { return m0 + i / MT * 128 + (wm * MT + i % MT) * 16 + c; };
+        auto read = [&](int i) { return out.row(p, min(row_of(i), (int64_t)p.M - 1)); };
+        typename Output::Row next = read(0);
 #pragma unroll
         for (int i = 0; i < HALVES * MT; ++i) {
-            const int64_t m = m0 + i / MT * 128 + (wm * MT + i % MT) * 16 + c;
-            if (m >= p.M) continue;
-            Acc first[RUN / 4], second[RUN / 4];
+            const typename Output::Row now = next;
+            if (i + 1 < HALVES * MT) next = read(i + 1);
+            if (row_of(i) < p.M) {
+                Acc first[RUN / 4], second[RUN / 4];
 #pragma unroll
-            for (int t = 0; t < RUN / 4; ++t) {
-                first[t] = acc[i][u + t];
-                second[t] = acc[i][GATED ? 2 + t : u + t];
+                for (int t = 0; t < RUN / 4; ++t) {
+                    first[t] = acc[i][u + t];
+                    second[t] = acc[i][GATED ? 2 + t : u + t];
+                }
+                out.store(p, row_of(i), now, first, second);
             }
-            out.store(p, m, first, second);
+            if constexpr (TILE_N == 256) __builtin_amdgcn_sched_barrier(0);  // (more rows at a time do not fit the registers)
         }
     }
 }

@@ -59,7 +59,7 @@ bool product_tiles_ok(bool bits8, rtoss_dtype out, const Product& p);
 constexpr struct { int rows, channels; } kTiles[3] = {{128, 128}, {256, 128}, {256, 256}};
 rtoss_status launch_product_tiles(ProductForm form, bool bits8, rtoss_dtype out, int tile, const Product& p, hipStream_t s);
 // ... of few tiles, and fp32: the sum split over the waves of a workgroup (product_slices.hip).  The tile, rows x channels of a matrix: kSlices;
-// gradients take the last.
+// gradients take the last.  kSliceTiles: the last, one for every wave (fp32, kGated).
 constexpr int kSliceTiles = 5;
 constexpr int kMaxSliceTiles = 0xffffffff / 512 / 16 * 8;  // (half of what a grid of 512 lanes each may have)
 constexpr struct { int rows, channels, gated; } kSlices[kSliceTiles] = {{16, 16, 16}, {32, 16, 16}, {32, 32, 32}, {64, 32, 16}, {64, 64, 32}};

@@ -80,11 +80,13 @@ rtoss_status gated_desc(const rtoss_gated_desc* desc, rtoss_gated_desc* d)
 //   slices of a x b: the launch 3.1, then for each round a little more the larger the tile, and the rows of both operands at 72, 41, 37 KB/us and CU
 //     (fp32 also 0.77e6 products), or where the sum is short a workgroup's beginning and end.  8-bit 4096 x 4096, rows 1, 64, 128, 256: 5.2, 6.7,
 //     7.6, 9.9 with the tile that this takes; 8.4, 9.4, 9.4, 9.9 with 64 x 64 for all.
+//   slices of 64 x 64, one for every wave (fp32): 4.5, then for each round 4, 6 and 2.85, 3.6 a stage.  Gated fp32 16 -> 2801, rows 300, 1453, 6000:
+//     8, 12, 44, a workgroup for each 11, 39, 146; 333 -> 2801 41, 48, 212 and 23, 84, 334; 2048 -> 2801 159, 186, 849 and 53, 210, 828.
 //   tiles: for each round 6, 6, 7 and 0.85, 1.2, 1.8 a stage of 128 bytes; 0.77 and 0.65 of that with 128 rows, 8.9 and 1.26 with 256 channels.
 //     Gated bf16 4096 -> 10944, rows 128, 256, 512, 1024, 2048: 49, 83, 118, 224, 420 with 128 x 128; 58, 62, 117, 184, 351 with 256 x 128; 80, 83,
 //     88, 176, 287 with 256 x 256; slices of 64 x 64 63, 105, 183, 335, 635.
 struct Choice {
-    int kernel;   // slices by tile, then tiles
+    int kernel;   // slices by tile, those of a tile for every wave, tiles
     double time;  // us
 };
 Choice choose(ProductForm form, bool bits8, rtoss_dtype out, const Product& p, int cus)
@@ -108,6 +110,11 @@ Choice choose(ProductForm form, bool bits8, rtoss_dtype out, const Product& p, i
         const double time = 3.1 + rounds * std::max(sum, kShort[t] * kAligned[rows] * (gated ? 1.85 : 1) * (eb == 4 ? 1.24 : 1));
         if (time < best.time) best = Choice{t, time};
     }
+    if (eb == 4 && gated) {
+        const double rounds = std::ceil(tiles(64, 32) / (8 * cus)), stages = std::ceil(row / 128);
+        const double time = 4.5 + rounds * (rows == kWhole ? 4 + stages * 2.85 : 6 + stages * 3.6);
+        if (time < best.time) best = Choice{kSliceTiles, time};
+    }
     if (product_tiles_ok(bits8, out, p)) {
         constexpr double kStageTime[] = {0.85, 1.2, 1.8}, kRoundTime[] = {6, 6, 7};
         const double stages = std::ceil(row / 128);
@@ -115,7 +122,7 @@ Choice choose(ProductForm form, bool bits8, rtoss_dtype out, const Product& p, i
             const double rounds = std::ceil(tiles(kTiles[t].rows, kTiles[t].channels / (gated ? 2 : 1)) / cus);
             const double one = t == 2 ? 8.9 + stages * 1.26 : kRoundTime[rows] * (t ? 1 : 0.77) + stages * kStageTime[rows] * (t ? 1 : 0.65);
             const double time = rounds * one;
-            if (time < best.time) best = Choice{kSliceTiles + t, time};
+            if (time < best.time) best = Choice{kSliceTiles + 1 + t, time};
         }
     }
     return best;
@@ -123,8 +130,8 @@ Choice choose(ProductForm form, bool bits8, rtoss_dtype out, const Product& p, i
 
 rtoss_status launch_chosen(int kernel, ProductForm form, bool bits8, rtoss_dtype out, const Product& p, hipStream_t s)
 {
-    if (kernel < kSliceTiles) return launch_product_slices(form, bits8, out, kernel, p, s);
-    return launch_product_tiles(form, bits8, out, kernel - kSliceTiles, p, s);
+    if (kernel <= kSliceTiles) return launch_product_slices(form, bits8, out, kernel, p, s);
+    return launch_product_tiles(form, bits8, out, kernel - kSliceTiles - 1, p, s);
 }
 
 // A launch has at most kMaxSliceTiles of the largest slices: more rows than that take several.
