@@ -54,23 +54,21 @@ template <typename TO, int N> __device__ __forceinline__ void store_run(TO* p, c
         }
     }
 }
-template <typename TO, int N> struct Run {
-    TO of[N];
-};
-template <typename TO, int N> __device__ __forceinline__ Run<TO, N> load_run(const TO* p, int left, Runs runs)
+template <typename TO, int N> __device__ __forceinline__ void add_run(const TO* p, float (&v)[N], int left, Runs runs)
 {
-    Run<TO, N> t;
     if (left >= N && (sizeof(TO) == 4 || runs != kRunElements)) {
-        __builtin_memcpy(t.of, __builtin_assume_aligned(p, 4), sizeof t);
-    } else {
+        TO t[N];
+        __builtin_memcpy(t, __builtin_assume_aligned(p, 4), sizeof t);
 #pragma unroll
-        for (int i = 0; i < N; ++i) t.of[i] = p[min(i, left - 1)];
+        for (int i = 0; i < N; ++i) v[i] += to_f32(t[i]);
+        return;
     }
-    return t;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        if (i < left) v[i] += to_f32(p[i]);
 }
 
-// The stage for channels n .. n+RUN-1 (n < N) of any rows.  What it reads of a row is asked for apart, so that it can be read before other rows are
-// stored: a wait for a load is one for all stores before it.
+// The stage for channels n .. n+RUN-1 of any rows.
 template <int FORM, typename T, typename TO, int RUN> struct RunOutput {
     static constexpr bool kScales = sizeof(T) == 1;
     typedef typename AccOf<T>::type Acc;
@@ -99,21 +97,10 @@ template <int FORM, typename T, typename TO, int RUN> struct RunOutput {
             if constexpr (kScales) v[i] = v[i] * sa * s[i];
         }
     }
-    struct Row {
-        float sa;
-        Run<TO, FORM == kScaled ? RUN : 1> residual;
-    };
-    __device__ __forceinline__ Row row(const Product& p, int64_t m) const  // m < M
+    // A row's scale, read before other rows are stored: a wait for a load is one for all stores before it.
+    static __device__ __forceinline__ float scale(const Product& p, int64_t m) { return kScales && p.sa ? p.sa[min(m, (int64_t)p.M - 1)] : 1.f; }
+    __device__ __forceinline__ void store(const Product& p, int64_t m, float sa, const Acc (&first)[RUN / 4], const Acc (&second)[RUN / 4]) const
     {
-        Row r;
-        r.sa = kScales && p.sa ? p.sa[m] : 1.f;
-        if constexpr (FORM == kScaled)
-            if (p.residual) r.residual = load_run<TO, RUN>((const TO*)p.residual + m * p.ldr + n, left, residual);
-        return r;
-    }
-    __device__ __forceinline__ void store(const Product& p, int64_t m, const Row& row, const Acc (&first)[RUN / 4], const Acc (&second)[RUN / 4]) const
-    {
-        const float sa = row.sa;
         float v[RUN];
         values(v, first, s0, sa);
         if constexpr (FORM == kScaled) {
@@ -121,9 +108,7 @@ template <int FORM, typename T, typename TO, int RUN> struct RunOutput {
 #pragma unroll
                 for (int i = 0; i < RUN; ++i) v[i] += bias[i];
             gate_act<RUN>(v, p.act);
-            if (p.residual)
-#pragma unroll
-                for (int i = 0; i < RUN; ++i) v[i] += to_f32(row.residual.of[i]);
+            if (p.residual) add_run<TO, RUN>((const TO*)p.residual + m * p.ldr + n, v, left, residual);
         } else if constexpr (FORM == kGated) {
             float u[RUN];
             values(u, second, s1, sa);

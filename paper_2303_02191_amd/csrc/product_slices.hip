@@ -161,10 +161,10 @@ __device__ __forceinline__ void product_slices(Product p, int work, int tiles_m,
         return n0 + (B_ACROSS ? (PART * share + u) * 16 + 4 * q : GATED ? 2 * NT * q + 4 * share : 4 * NT * q + 4 * PART * share);
     };
     typedef RunOutput<FORM, T, TO, RUN> Output;
-    auto read_of = [&](const Output& out, int unit) { return out.row(p, min(row_of(unit), (int64_t)p.M - 1)); };
+    auto scale_of = [&](int unit) { return Output::scale(p, row_of(unit)); };
     const int first_unit = EACH ? 0 : wave;
     const Output first_out(p, min(channel_of(first_unit, 0), p.N - 1));  // (across: it holds nothing but the place)
-    const auto first_read = read_of(first_out, first_unit);
+    const float first_scale = scale_of(first_unit);
 
     auto read_and_multiply = [&](const char* base, int s, auto&& then) {
         u32x4 af[2][MT], bf[2][NT];
@@ -283,7 +283,7 @@ __device__ __forceinline__ void product_slices(Product p, int work, int tiles_m,
     struct Sum {
         Acc of[PART];
     };
-    auto finish = [&](int unit, const Output& out, const typename Output::Row& read, const Sum& of) {
+    auto finish = [&](int unit, const Output& out, float sa, const Sum& of) {
         const auto& sum = of.of;
         const int64_t m = row_of(unit);
         if (m >= p.M) return;
@@ -293,18 +293,17 @@ __device__ __forceinline__ void product_slices(Product p, int work, int tiles_m,
             if (n >= p.N) continue;
             if constexpr (B_ACROSS) {
                 const Acc one[1] = {sum[u]};
-                Output(p, n).store(p, m, read, one, one);
+                Output(p, n).store(p, m, sa, one, one);
             } else if constexpr (GATED) {
                 const Acc first[1] = {sum[0]}, second[1] = {sum[PART - 1]};
-                out.store(p, m, read, first, second);
+                out.store(p, m, sa, first, second);
             } else {
-                out.store(p, m, read, sum, sum);
+                out.store(p, m, sa, sum, sum);
             }
         }
     };
     auto finish_next = [&](int unit, const Sum& sum) {
-        const Output out(p, min(channel_of(unit, 0), p.N - 1));
-        finish(unit, out, read_of(out, unit), sum);
+        finish(unit, Output(p, min(channel_of(unit, 0), p.N - 1)), scale_of(unit), sum);
     };
     if constexpr (EACH) {
         static_for<UNITS>([&](auto which) {
@@ -312,7 +311,7 @@ __device__ __forceinline__ void product_slices(Product p, int work, int tiles_m,
             Sum sum;
 #pragma unroll
             for (int t = 0; t < PART; ++t) sum.of[t] = acc[unit / SHARE][GATED ? NT / 2 * t + share : PART * share + t];
-            if constexpr (unit == 0) finish(unit, first_out, first_read, sum);
+            if constexpr (unit == 0) finish(unit, first_out, first_scale, sum);
             else finish_next(unit, sum);
         });
         return;
@@ -368,7 +367,7 @@ __device__ __forceinline__ void product_slices(Product p, int work, int tiles_m,
             return;
         }
     }
-    if (wave < UNITS) finish(wave, first_out, first_read, sum_of(wave));
+    if (wave < UNITS) finish(wave, first_out, first_scale, sum_of(wave));
     for (int unit = wave + WAVES; unit < UNITS; unit += WAVES) finish_next(unit, sum_of(unit));
 }
 

@@ -290,12 +290,11 @@ __global__ __launch_bounds__(512, 2) void product_tiles_kernel(Product p, int ti
         typedef RunOutput<FORM, T, TO, RUN> Output;
         const Output out(p, n);
         auto row_of = [&](int i) { return m0 + i / MT * 128 + (wm * MT + i % MT) * 16 + c; };
-        auto read = [&](int i) { return out.row(p, min(row_of(i), (int64_t)p.M - 1)); };
-        typename Output::Row next = read(0);
+        float next = Output::scale(p, row_of(0));
 #pragma unroll
         for (int i = 0; i < HALVES * MT; ++i) {
-            const typename Output::Row now = next;
-            if (i + 1 < HALVES * MT) next = read(i + 1);
+            const float sa = next;
+            if (i + 1 < HALVES * MT) next = Output::scale(p, row_of(i + 1));
             if (row_of(i) < p.M) {
                 Acc first[RUN / 4], second[RUN / 4];
 #pragma unroll
@@ -303,9 +302,8 @@ __global__ __launch_bounds__(512, 2) void product_tiles_kernel(Product p, int ti
                     first[t] = acc[i][u + t];
                     second[t] = acc[i][GATED ? 2 + t : u + t];
                 }
-                out.store(p, row_of(i), now, first, second);
+                out.store(p, row_of(i), sa, first, second);
             }
-            if constexpr (TILE_N == 256) __builtin_amdgcn_sched_barrier(0);  // (more rows at a time do not fit the registers)
         }
     }
 }
