@@ -345,6 +345,58 @@ def test_long_sums_have_one_order(M, K, F, dt):
             equal(a, b, "call %d" % i)
 
 
+# many tiles of short sums: of the gradients, of the weights' or the rows', and of the gated block
+SHORT = [(20, 1030, 2100), (4300, 1040, 100), (1500, 16, 2801), (2600, 70, 1500)]
+
+
+@pytest.mark.parametrize("pitch", [0, 3])
+@pytest.mark.parametrize("dt", list(DT))
+@pytest.mark.parametrize("M,K,F", SHORT)
+def test_many_short_sums(M, K, F, dt, pitch):
+    """Whole numbers: projections of at most K, whose product is below 2^24, and sums of at most 4 (M + 2 F), all exact in 32 bits."""
+    g = gen(M + 11 * K + F + pitch)
+    t = DT[dt]
+    x, _ = inside(whole(g, (M, K), 1, t), pitch, float("nan"))
+    wg, _ = inside(whole(g, (F, K), 1, t), pitch, float("nan"))
+    wu, _ = inside(whole(g, (F, K), 1, t), pitch, float("nan"))
+    dh, _ = inside(whole(g, (M, F), 2, t), pitch, float("nan"))
+    gate, up = whole(g, (M, F), 2, t), whole(g, (M, F), 2, t)
+    wide = x.double() @ wg.double().t()
+    other = x.double() @ wu.double().t()
+    h, kept, kept_up = pl.gated_ff(x, wg, wu, act=1, keep=True)
+    equal(kept, wide.to(t), "gate")
+    equal(kept_up, other.to(t), "up")
+    equal(h, (torch.relu(wide) * other).to(t), "h")
+    dg, du = dh.double() * up.double(), dh.double() * gate.double()
+    dx, dwg, dwu = pl.gated_ff_backward(dh, x, wg, wu, gate, up, act=0)
+    equal(dx, (dg @ wg.double() + du @ wu.double()).to(t), "dx")
+    equal(dwg, (dg.t() @ x.double()).to(t), "dw_gate")
+    equal(dwu, (du.t() @ x.double()).to(t), "dw_up")
+
+
+@pytest.mark.parametrize("ld", [(1 << 24) + 16, (1 << 24) + 4, (1 << 24) + 3])
+def test_rows_far_apart(ld):
+    """Rows 16 MB and more from one another (in bytes; 16-bit ones half as many elements): a tile is larger than offsets of 31 bits."""
+    g = gen(91)
+    M, K, N = 130, 100, 20
+
+    def far(t, ld):
+        buf = torch.zeros((t.shape[0] - 1) * ld + t.shape[1], dtype=t.dtype, device="cuda")
+        view = buf.as_strided(t.shape, (ld, 1))
+        view.copy_(t)
+        return view
+
+    a, w = codes(g, (M, K)), codes(g, (N, K))
+    equal(pl.matmul_i8(far(a, ld), None, far(w, ld), None, out_dt=B.F32), (a.double() @ w.double().t()).float())
+    x, wg, wu = (whole(g, shape, 1, torch.bfloat16) for shape in ((M, K), (N, K), (N, K)))
+    gate, up, dh = (whole(g, (M, N), 2, torch.bfloat16) for _ in range(3))
+    half = ld // 2 + 1
+    want = pl.gated_ff_backward(dh, x, wg, wu, gate, up)
+    for got, plain in zip(pl.gated_ff_backward(dh, far(x, half), far(wg, half), far(wu, half), gate, up), want):
+        equal(got, plain)
+    equal(pl.gated_ff(far(x, half), far(wg, half), far(wu, half), act=1), pl.gated_ff(x, wg, wu, act=1))
+
+
 def _silu_slope(v):
     s = torch.sigmoid(v)
     return s * (1 + v * (1 - s))
