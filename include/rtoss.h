@@ -352,11 +352,15 @@ rtoss_status rtoss_conv2d_pattern_coherent(const rtoss_wdesc* desc, const rtoss_
  * Common to the calls below
  *   - A pitch (x_ld, a_ld, w_ld, h_ld, q_ld) is the number of elements from one row's first to the next row's; 0 means a
  *     plain matrix.  A larger one makes the matrix a slice of a wider buffer (two weight matrices stored in one, the
- *     channels of a concatenation); what lies between the rows is neither read nor written.  Pointers and pitches need
- *     only the alignment of their elements; rows of whole 16-byte pieces that start at multiples of 16 bytes are the fast path.
+ *     channels of a concatenation); what lies between the rows may be read, but has no effect, and is not written.
+ *     Pointers and pitches need only the alignment of their elements; rows of whole 16-byte pieces that start at multiples of
+ *     16 bytes are the fast path, rows that start at multiples of 4 the next.
  *   - Rows 0 <= M < 2^31 (M = 0: nothing to do, row pointers may be NULL), channels 1 .. 2^24, pitches below 2^31 elements.
  *   - Results may not overlap operands or each other (checked for plain matrices).
- *   - Determinism: as above; no atomics, one order of additions for a shape, a type and the operands' alignment.
+ *   - Determinism: as above; one order of additions for a shape, a type, the operands' alignment and pitches and the number
+ *     of the device's CUs.
+ *   - Sums of 32-bit floats are formed of bf16 parts, to 32-bit precision; an infinite operand makes the sums that it enters NaN.
+ *     Of the 16-bit types it makes them what the type's arithmetic does.
  */
 
 /*
@@ -419,14 +423,16 @@ rtoss_status rtoss_gated_ff_i8(const rtoss_gated_desc* desc, const int8_t* a_dev
 
 /*
  * Gradients of rtoss_gated_ff from that of h:
- *     dg = dh * u * act'(g),  du = dh * act(g)     (in fp32, then rounded to dt; act' of ReLU at 0 is 0)
+ *     dg = dh * u * act'(g),  du = dh * act(g)     (in fp32, then rounded to dt, in whose range they have to lie; act' of ReLU
+ *                                                   at 0 is 0)
  *     dx = dg w_gate + du w_up,   dw_gate = dg^T x,   dw_up = du^T x     (sums in fp32, rounded once)
  *
  *   dh_dev                  M x F, pitch h_ld          gate_dev, up_dev  as rtoss_gated_ff kept them
  *   dx_dev                  out: plain [M][K], or NULL (not computed; the weights may then be NULL)
  *   dw_gate_dev, dw_up_dev  out: plain [F][K], or both NULL (x may then be NULL).  Of no rows (M = 0) they are zero.
  *   workspace_dev           scratch of the size that rtoss_gated_ff_backward_size gives for the descriptor (host only, no GPU
- *                           needed), 256-byte aligned; it holds nothing between calls
+ *                           needed), 256-byte aligned; it holds nothing between calls, and calls that may run at the same time
+ *                           need one each
  * Errors: RTOSS_EDTYPE, RTOSS_ESHAPE, RTOSS_EINVAL, RTOSS_ENOSPACE.
  */
 rtoss_status rtoss_gated_ff_backward_size(const rtoss_gated_desc* desc, size_t* workspace_bytes);

@@ -1,29 +1,30 @@
-// Products of whole 16-byte pieces in tiles of 256 x 256 results: the 8-bit product, the gated block and its gradients where there are
-// rows enough.  Bound: the matrix instructions.
+// Products in tiles of 256 x 256, 256 x 128 and 128 x 128 results: the 8-bit product, the gated block and its gradients where there are rows
+// enough.  Bound: the matrix instructions.
 //
-// A workgroup is eight waves, two per SIMD; wave (wm, wn) of 2 x 4 owns 128 x 64 results (128 accumulator registers).  The sum runs over
-// stages of 128 bytes of a row, two buffers of 64 KB in LDS, each in four regions: the halves of the left and of the right operand.  A
-// stage is four quadrants (half of the wave's rows x half of its channels, 16 matrix instructions for two steps of the sum), and a
-// quadrant two parts with a barrier behind each: reading operands and starting copies, and multiplying.  The waves of wm = 1 run one
-// part behind those of wm = 0, so that on every SIMD one wave multiplies while the other reads.
-//   - Quadrants run (0, x) (0, y) (1, y) (1, x); x is the half whose operands are there from the stage before, where they were read
-//     beside the last quadrant into the registers of y.  So a quadrant reads 8, 4, 8, 4 vectors of 1 KB a wave, 256 cycles of LDS at most
-//     for four waves, beside 256 cycles of matrix instructions.
-//   - Number the quadrants p and the regions in the order of their use, j (x of B, half 0 of A, y of B, half 1 of A): p reads
-//     region p + 1 and starts the copies of p + 7, whose place the region p - 1 had, read in quadrant p - 2: its reads were waited for by
-//     both groups of waves a barrier ago.  A region has six quadrants, some 3000 cycles, to arrive; the wait of quadrant p covers
-//     region p + 2, in front of a barrier of both groups that precedes its reads.
+// A workgroup is eight waves, two per SIMD; of 256 x 256 results wave (wm, wn) of 2 x 4 owns 128 x 64 (128 accumulator registers), of
+// 256 x 128 or 128 x 128 one of 4 x 2 owns 64 x 64 or 32 x 64.  The sum runs over stages of 128 bytes of a row, in buffers in LDS of regions of
+// 16 KB: the halves of the left operand's rows, and one or two of the right one.  A stage is two parts (128 rows: one), in each of which a
+// wave reads operands, of half of its rows, and multiplies them, with a barrier behind either.  The waves of the second four run half a
+// part behind the first, so that on every SIMD one wave multiplies while the other reads.
+//   - A wave holds the right operand of a stage for both parts, so that the first reads 8 + 8 vectors of 1 KB (256 x 128: 8 + 4) and the
+//     second 8 (4), beside 64 (32) matrix instructions each.
+//   - Two buffers: a stage's first part starts the copies of the second half of the rows for the next stage, the second those of all else for the
+//     stage after that.  Every place has been read by both halves of the waves a barrier before; a region has a stage and a half to
+//     arrive, and the wait in front of a part's barrier covers what the next part reads, whoever copied it.
+//   - 128 rows: four buffers, copies three stages ahead.
 // Behind the last stage the last one is copied again into free regions, so that every wait can count copies.
 //
 // Operands that memory holds by rows of the sum's direction (weights and rows of the forward pass) lie in LDS as rows of 128 bytes, those
 // that it holds across (weights in the gradient of the rows; both in that of the weights) as 128 columns of each of the stage's
 // rows, and are transposed by the read (ds_read_b64_tr_b16: lane 4k + j of 16 gives the address of four columns, lane i gets
-// column i of the four rows that lanes 4k .. 4k+3 name, k = 0 .. 3; fp32: one element per read).  Pieces of 16 bytes are
-// exchanged within a row so that the reads spread over the banks.
+// column i of the four rows that lanes 4k .. 4k+3 name, k = 0 .. 3).  Pieces of 16 bytes are exchanged within a row so that the reads spread
+// over the banks.  Rows that are no whole pieces come through registers (product_words.h), in tiles of 128 channels.
 //
-// Measured: 8-bit 8192 x 8192 x 8192 with residual 447 us (2.46 POP/s; a library product without the output stage 2.06), gated block bf16
-// 8192 rows x 4096 -> 10944 with both projections kept 1143 us (1.28 PFLOP/s, 1.5 is what a library product of 8192^3 reaches), its gradients
-// with dg and du 2521 us (1.17 PFLOP/s; library products of operands that lie across 1.17 and 1.03).
+// Measured: 8-bit 8192 x 8192 x 8192 403 us (2.73 POP/s; a library product 2.06; matrix instructions with reads of LDS and nothing else
+// 3.3), gated block bf16 8192 rows x 4096 -> 10944 1040 us (1.41 PFLOP/s; a library product of 8192^3 1.5, instructions with reads 1.7), its
+// gradients with dg and du 2420 us (1.21 PFLOP/s; library products of operands that lie across 1.17 and 1.03).  A tile costs 6 to 9 us besides
+// its stages (its first copies, the output stage).  Workgroups that take several tiles and copy the next one's stages during the output
+// stage: 3 % faster at 8192 rows, 10 to 19 % slower where every workgroup has one, for what it takes to find the copies' place.
 #include <algorithm>
 
 #include "product_run.h"
