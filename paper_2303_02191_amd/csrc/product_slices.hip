@@ -95,7 +95,8 @@ __device__ __forceinline__ void product_slices(Product p, int work, int tiles_m,
     const Source b0 = B_ACROSS ? columns_from(p.b0, ldb, n0, p.N) : rows_from(p.b0, ldb, n0, p.N);
     const Source b1 = GATED ? rows_from(p.b1, ldb, n0, p.N) : FORM == kBackRows ? columns_from(p.b1, ldb, n0, p.N) : b0;
 
-    // ---- copies; a lane's channel is such that its results are neighbouring channels.  Gated: the second half of B's rows are w_up's ----
+    // ---- copies; a lane's channel is such that its results are neighbouring channels (gated: those of four
+    // neighbouring lanes are).  Gated: the second half of B's rows are w_up's ----
     typedef Across<T, 64> AcrossA, AcrossB;
     static_assert((!A_ACROSS || BM == 64) && (!B_ACROSS || BN == 64), "operands that lie across");
     const int sub = lane >> 3, piece = (lane & 7) ^ sub;
@@ -117,9 +118,8 @@ __device__ __forceinline__ void product_slices(Product p, int work, int tiles_m,
             const int r = k * AcrossB::kCopyRows + lane / AcrossB::kPieces;
             vb[i] = (uint32_t)r * (uint32_t)ldb + (lane % AcrossB::kPieces ^ AcrossB::spread(r)) * 16;
         } else {
-            constexpr int TILES = GATED ? NT / 2 : NT;  // of a wave and matrix
             const int rho = (k * 8 + sub) % COLS, t = rho / 16, r = rho & 15;
-            vb[i] = (uint32_t)(4 * TILES * (r >> 2) + 4 * t + (r & 3)) * (uint32_t)ldb + piece * 16;
+            vb[i] = (uint32_t)(GATED ? rho : 4 * NT * (r >> 2) + 4 * t + (r & 3)) * (uint32_t)ldb + piece * 16;
         }
     }
     char* const own = smem + wave * BUFFER;
@@ -164,7 +164,7 @@ __device__ __forceinline__ void product_slices(Product p, int work, int tiles_m,
     auto row_of = [&](int unit) { return m0 + unit / SHARE * 16 + c; };
     auto channel_of = [&](int unit, int u) {
         const int share = unit % SHARE;
-        return n0 + (B_ACROSS ? (PART * share + u) * 16 + 4 * q : GATED ? 2 * NT * q + 4 * share : 4 * NT * q + 4 * PART * share);
+        return n0 + (B_ACROSS ? (PART * share + u) * 16 + 4 * q : GATED ? 16 * share + 4 * q : 4 * NT * q + 4 * PART * share);
     };
     typedef RunOutput<FORM, T, TO, RUN> Output;
     auto scale_of = [&](int unit) { return Output::scale(p, row_of(unit)); };
@@ -263,9 +263,8 @@ __device__ __forceinline__ void product_slices(Product p, int work, int tiles_m,
                 const bool of_a = i < A_COPIES;
                 const int k = of_a ? i : i - A_COPIES, r = of_a ? k * (64 / PA) + lane / PA : k * (64 / PB) + lane / PB;
                 if (of_a || B_ACROSS) return r;
-                constexpr int TILES = GATED ? NT / 2 : NT;
                 const int in = r % COLS;
-                return 4 * TILES * ((in & 15) >> 2) + 4 * (in / 16) + (in & 3);
+                return GATED ? in : 4 * NT * ((in & 15) >> 2) + 4 * (in / 16) + (in & 3);
             }
             static __device__ __forceinline__ int column(int) { return 0; }
             static __device__ __forceinline__ bool up(int i) { return GATED && i - A_COPIES >= B_COPIES / 2; }
@@ -376,7 +375,8 @@ __device__ __forceinline__ void product_slices(Product p, int work, int tiles_m,
         }
     }
     if (wave < UNITS) finish(wave, first_out, first_scale, sum_of(wave));
-    for (int unit = wave + WAVES; unit < UNITS; unit += WAVES) finish_next(unit, sum_of(unit));
+    if constexpr (UNITS > WAVES)
+        for (int unit = wave + WAVES; unit < UNITS; unit += WAVES) finish_next(unit, sum_of(unit));
 }
 
 template <typename T, typename TO, int FORM, int ROWS, int BM, int BN, int WAVES, bool EACH>
