@@ -79,7 +79,7 @@ template <int FORM, typename T, typename TO, int RUN> struct RunOutput {
     __device__ __forceinline__ RunOutput(const Product& p, int n_) : n(n_), left(p.N - n_)
     {
         runs = runs_of<TO>(p.y, p.ldy);
-        kept = runs_of<TO>((const void*)((uintptr_t)p.y0 | (uintptr_t)p.y1), p.N);
+        kept = runs_of<TO>((const void*)((uintptr_t)p.y0 | (uintptr_t)p.y1), p.ldk);
         residual = runs_of<TO>(p.residual, p.ldr);
 #pragma unroll
         for (int i = 0; i < RUN; ++i) {
@@ -113,8 +113,8 @@ template <int FORM, typename T, typename TO, int RUN> struct RunOutput {
             float u[RUN];
             values(u, second, s1, sa);
             if (p.y0) {
-                store_run<TO, RUN>((TO*)p.y0 + m * p.N + n, v, left, kept);
-                store_run<TO, RUN>((TO*)p.y1 + m * p.N + n, u, left, kept);
+                store_run<TO, RUN>((TO*)p.y0 + m * p.ldk + n, v, left, kept);
+                store_run<TO, RUN>((TO*)p.y1 + m * p.ldk + n, u, left, kept);
             }
             gate_act<RUN>(v, p.act);
 #pragma unroll

@@ -23,7 +23,7 @@ struct Product {
     const float *sa, *s0, *s1, *bias;  // nullptr: 1, 1, 1, 0
     const void* residual;
     void *y, *y0, *y1;  // kGated: y0, y1 keep g and u, or nullptr
-    int64_t ldr, ldy;   // of residual and y (y0 and y1 are plain)
+    int64_t ldr, ldy, ldk;  // of residual, y and what is kept (kBackWeights: ldy of both)
 };
 
 // ReLU keeps a NaN, as the plain comparison does (a row that could not be quantized stays visible); SiLU: epilogue.h.

@@ -134,28 +134,88 @@ rtoss_status launch_chosen(int kernel, ProductForm form, bool bits8, rtoss_dtype
     return launch_product_tiles(form, bits8, out, kernel - kSliceTiles - 1, p, s);
 }
 
+// Rows m .. m+rows-1 of the result, and channels n .. n+channels-1.
+void* on(const void* base, int64_t bytes) { return base ? (void*)((char*)base + bytes) : nullptr; }
+Product rows_of(ProductForm form, int eb, int out_eb, const Product& p, int64_t m, int64_t rows)
+{
+    Product part = p;
+    const int64_t a_step = form == kBackWeights ? eb : p.lda * eb;  // (there the rows of the result are columns of its operand)
+    part.M = (int)rows;
+    part.a0 = on(p.a0, m * a_step);
+    part.a1 = on(p.a1, m * a_step);
+    part.sa = (const float*)on(p.sa, m * 4);
+    part.residual = on(p.residual, m * p.ldr * out_eb);
+    part.y = on(p.y, m * p.ldy * out_eb);
+    part.y0 = on(p.y0, m * p.ldk * out_eb);
+    part.y1 = on(p.y1, m * (form == kBackWeights ? p.ldy : p.ldk) * out_eb);
+    return part;
+}
+Product channels_of(ProductForm form, int eb, int out_eb, const Product& p, int64_t n, int64_t channels)
+{
+    Product part = p;
+    const int64_t b_step = form == kBackRows || form == kBackWeights ? eb : p.ldb * eb;
+    part.N = (int)channels;
+    part.b0 = on(p.b0, n * b_step);
+    part.b1 = on(p.b1, n * b_step);
+    part.s0 = (const float*)on(p.s0, n * 4);
+    part.s1 = (const float*)on(p.s1, n * 4);
+    part.bias = (const float*)on(p.bias, n * 4);
+    part.residual = on(p.residual, n * out_eb);
+    part.y = on(p.y, n * out_eb);
+    part.y0 = on(p.y0, n * out_eb);
+    part.y1 = on(p.y1, n * out_eb);
+    return part;
+}
+
+// A product in one launch, or in two: as many rows or channels as fill whole rounds of tiles, and the rest with what suits it, where that is
+// shorter.  Gated bf16 1000 x 4096 -> 10944: 344 tiles of 256 x 256, two rounds, 176 us; 256 of them, and the last 2752 channels in 172 of
+// 256 x 128, 161.
+struct ProductPlan {
+    double time;
+    int64_t rows, channels;  // of the first launch
+};
+ProductPlan plan_product(ProductForm form, bool bits8, rtoss_dtype out, const Product& p, int cus)
+{
+    const int eb = bits8 ? 1 : elem_bytes(out), out_eb = elem_bytes(out);
+    const Choice whole = choose(form, bits8, out, p, cus);
+    ProductPlan best{whole.time, p.M, p.N};
+    if (whole.kernel <= kSliceTiles) return best;
+    const auto& tile = kTiles[whole.kernel - kSliceTiles - 1];
+    const int width = form == kGated ? tile.channels / 2 : tile.channels, both = form == kBackWeights ? 2 : 1;
+    const int64_t high = ((int64_t)p.M + tile.rows - 1) / tile.rows, wide = ((int64_t)p.N + width - 1) / width, tiles = high * wide * both;
+    const int64_t full = (tiles - 1) / cus * cus;  // tiles of whole rounds, without the last
+    const auto try_split = [&](const Product& first, const Product& rest, int64_t rows, int64_t channels) {
+        const double time = choose(form, bits8, out, first, cus).time + choose(form, bits8, out, rest, cus).time + 1.5;
+        if (time < best.time * 0.97) best = ProductPlan{time, rows, channels};
+    };
+    const int64_t rows = full / (wide * both) * tile.rows, channels = full / (high * both) * width;
+    if (rows > 0 && rows < p.M) try_split(rows_of(form, eb, out_eb, p, 0, rows), rows_of(form, eb, out_eb, p, rows, p.M - rows), rows, p.N);
+    if (channels > 0 && channels < p.N)
+        try_split(channels_of(form, eb, out_eb, p, 0, channels), channels_of(form, eb, out_eb, p, channels, p.N - channels), p.M, channels);
+    return best;
+}
+
 // A launch has at most kMaxSliceTiles of the largest slices: more rows than that take several.
 rtoss_status launch_product(ProductForm form, bool bits8, rtoss_dtype out, const Product& p, hipStream_t s)
 {
     DeviceInfo dev;
     RTOSS_TRY(current_device(&dev));
     const int eb = bits8 ? 1 : elem_bytes(out), out_eb = elem_bytes(out);
+    const auto launch = [&](const Product& part) { return launch_chosen(choose(form, bits8, out, part, dev.cus).kernel, form, bits8, out, part, s); };
     const int64_t across = ((int64_t)p.N + 31) / 32 * 2;
     const int64_t most = std::max<int64_t>(kMaxSliceTiles / across, 1) * 64;  // rows
-    if (p.M <= most) return launch_chosen(choose(form, bits8, out, p, dev.cus).kernel, form, bits8, out, p, s);
     for (int64_t m = 0; m < p.M; m += most) {
-        Product part = p;
-        const auto on = [](const void* base, int64_t bytes) { return base ? (void*)((char*)base + bytes) : nullptr; };
-        const int64_t a_step = form == kBackWeights ? eb : p.lda * eb;  // (there the rows of the result are columns of its operand)
-        part.M = (int)std::min<int64_t>(most, p.M - m);
-        part.a0 = on(p.a0, m * a_step);
-        part.a1 = on(p.a1, m * a_step);
-        part.sa = (const float*)on(p.sa, m * 4);
-        part.residual = on(p.residual, m * p.ldr * out_eb);
-        part.y = on(p.y, m * p.ldy * out_eb);
-        part.y0 = on(p.y0, m * p.N * out_eb);
-        part.y1 = on(p.y1, m * (form == kBackWeights ? p.ldy : p.N) * out_eb);
-        RTOSS_TRY(launch_chosen(choose(form, bits8, out, part, dev.cus).kernel, form, bits8, out, part, s));
+        const Product part = rows_of(form, eb, out_eb, p, m, std::min<int64_t>(most, p.M - m));
+        const ProductPlan plan = plan_product(form, bits8, out, part, dev.cus);
+        if (plan.rows < part.M) {
+            RTOSS_TRY(launch(rows_of(form, eb, out_eb, part, 0, plan.rows)));
+            RTOSS_TRY(launch(rows_of(form, eb, out_eb, part, plan.rows, part.M - plan.rows)));
+        } else if (plan.channels < part.N) {
+            RTOSS_TRY(launch(channels_of(form, eb, out_eb, part, 0, plan.channels)));
+            RTOSS_TRY(launch(channels_of(form, eb, out_eb, part, plan.channels, part.N - plan.channels)));
+        } else {
+            RTOSS_TRY(launch(part));
+        }
     }
     return RTOSS_OK;
 }
@@ -222,8 +282,8 @@ rtoss_status plan_gradients(rtoss_dtype dt, const Product& rows, const Product& 
     DeviceInfo dev;
     RTOSS_TRY(current_device(&dev));
     const int eb = elem_bytes(dt);
-    double two = choose(kBackWeights, false, dt, weights, dev.cus).time;
-    if (rows.M > 0) two += choose(kBackRows, false, dt, rows, dev.cus).time;
+    double two = plan_product(kBackWeights, false, dt, weights, dev.cus).time;
+    if (rows.M > 0) two += plan_product(kBackRows, false, dt, rows, dev.cus).time;
     const MergedSpeed& speed = merged_speed(dt, std::max(product_rows(kBackRows, rows, eb), product_rows(kBackWeights, weights, eb)));
     double best = 1e300;
     for (bool high : {false, true}) {
@@ -367,6 +427,7 @@ rtoss_status rtoss_gated_ff(const rtoss_gated_desc* desc, const void* x_dev, con
     p.y = h_dev;
     p.y0 = gate_dev;
     p.y1 = up_dev;
+    p.ldk = p.N;
     p.ldy = d.h_ld;
     return launch_product(kGated, false, d.dt, p, (hipStream_t)hip_stream);
 }

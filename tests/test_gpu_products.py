@@ -397,6 +397,40 @@ def test_rows_far_apart(ld):
     equal(pl.gated_ff(far(x, half), far(wg, half), far(wu, half), act=1), pl.gated_ff(x, wg, wu, act=1))
 
 
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+@pytest.mark.parametrize("M,K,N", [(1000, 1280, 9500), (17000, 1280, 1000), (1000, 1279, 9501)])
+def test_matmul_i8_of_more_than_whole_rounds(M, K, N, out):
+    """More tiles than the chip has CUs, the last of them in a launch of their own: of channels, of rows."""
+    g = gen(M + N)
+    a, w = codes(g, (M, K)), codes(g, (N, K))
+    sa, sw = whole(g, (M,), 2), whole(g, (N,), 2)
+    bias, residual = whole(g, (N,), 3), whole(g, (M, N), 3, DT[out])
+    y = pl.matmul_i8(a, sa, w, sw, bias=bias, residual=residual, out_dt=ABI[out])
+    sums = (a.double() @ w.double().t()).float()  # rounded once above 2^24; exact times 0, 1 and 2
+    want = (sums * sa[:, None] * sw + bias + residual.float()).to(DT[out])
+    equal(y, want)
+
+
+@pytest.mark.parametrize("dt", ["f16", "bf16"])
+@pytest.mark.parametrize("M,K,F", [(1000, 640, 9500), (1000, 641, 9501), (4100, 1030, 2760), (8200, 512, 2100)])
+def test_gated_ff_of_more_than_whole_rounds(M, K, F, dt):
+    """Projections of at most K; gradients' sums of at most 4 (M + 2 F)."""
+    g = gen(M + F)
+    t = DT[dt]
+    x, wg, wu = whole(g, (M, K), 1, t), whole(g, (F, K), 1, t), whole(g, (F, K), 1, t)
+    wide, other = x.double() @ wg.double().t(), x.double() @ wu.double().t()
+    h, gate, up = pl.gated_ff(x, wg, wu, act=1, keep=True)
+    equal(gate, wide.to(t), "gate")
+    equal(up, other.to(t), "up")
+    equal(h, (torch.relu(wide) * other).to(t), "h")
+    dh, gate, up = (whole(g, (M, F), 2, t) for _ in range(3))
+    dg, du = dh.double() * up.double(), dh.double() * gate.double()
+    dx, dwg, dwu = pl.gated_ff_backward(dh, x, wg, wu, gate, up, act=0)
+    equal(dx, (dg @ wg.double() + du @ wu.double()).to(t), "dx")
+    equal(dwg, (dg.t() @ x.double()).to(t), "dw_gate")
+    equal(dwu, (du.t() @ x.double()).to(t), "dw_up")
+
+
 def _silu_slope(v):
     s = torch.sigmoid(v)
     return s * (1 + v * (1 - s))
