@@ -36,15 +36,18 @@ void require(bool ok, const char* msg)
 {
     if (!ok) raise(PyExc_AssertionError, msg);
 }
-void check(rtoss_status st)
+[[noreturn]] void refuse(rtoss_status st, const char* msg)
 {
-    if (st == RTOSS_OK) return;
-    PyObject* e = PyObject_CallFunction(g_rtoss_error, "is", (int)st, rtoss_last_error());
+    PyObject* e = PyObject_CallFunction(g_rtoss_error, "is", (int)st, msg);
     if (e) {
         PyErr_SetObject(g_rtoss_error, e);
         Py_DECREF(e);
     }
     throw PyError{};
+}
+void check(rtoss_status st)
+{
+    if (st != RTOSS_OK) refuse(st, rtoss_last_error());
 }
 template <typename F> PyObject* guarded(F&& f)
 {
@@ -501,9 +504,16 @@ struct OnDevice {
     const at::Tensor& here(PyObject* o) const { return here(tensor(o)); }
 };
 void require_type(const at::Tensor& t, at::ScalarType st, const char* msg) { require(t.scalar_type() == st, msg); }
-int extent(int64_t v)  // (a size past the library's range is the library's error to report)
+int extent(int64_t channels)  // (past 2^24 they are the library's error to report)
 {
-    return (int)std::min<int64_t>(v, 0x7fffffff);
+    return (int)std::min<int64_t>(channels, 0x7fffffff);
+}
+// An epilogue's pitches are ints, all of whose values the library takes: one that is none is refused here.
+int pitch(const at::Tensor& t, const char* refusal)
+{
+    const int64_t ld = rows_of(t).ld;
+    if (ld > 0x7fffffff) refuse(RTOSS_ESHAPE, refusal);
+    return (int)ld;
 }
 const float* scales_arg(PyObject* o, int64_t n, const OnDevice& on)
 {
@@ -593,12 +603,12 @@ PyObject* py_matmul_i8(PyObject*, PyObject* const* a, Py_ssize_t n)
         e.scale_dev = scales_arg(a[3], rw.M, on);
         e.bias_dev = scales_arg(a[4], rw.M, on);
         e.act = (rtoss_act)integer(a[5]);
-        e.y_ld = extent(rows_of(y.t).ld);
+        e.y_ld = pitch(y.t, "y_ld is past 2^31 - 1");
         if (a[6] != Py_None) {
             const at::Tensor& res = on.here(a[6]);
             require(res.sizes() == y.t.sizes() && res.scalar_type() == y.t.scalar_type(), "residual must have y's shape and dtype");
             e.residual_dev = res.data_ptr();
-            e.residual_ld = extent(rows_of(res).ld);
+            e.residual_ld = pitch(res, "residual_ld is past 2^31 - 1");
         }
         const rtoss_matmul_desc d{r.M, extent(rw.M), extent(r.K), r.ld, rw.ld, (rtoss_dtype)out_dt};
         const auto *xp = (const int8_t*)x.data_ptr(), *wp = (const int8_t*)w.data_ptr();
