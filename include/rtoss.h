@@ -424,7 +424,7 @@ rtoss_status rtoss_gated_ff_i8(const rtoss_gated_desc* desc, const int8_t* a_dev
 /*
  * Gradients of rtoss_gated_ff from that of h:
  *     dg = dh * u * act'(g),  du = dh * act(g)     (in fp32, then rounded to dt, in whose range they have to lie; act' of ReLU
- *                                                   at 0 is 0)
+ *                                                   at 0 is 0, of a NaN a NaN; a zero times an infinity is a NaN here too)
  *     dx = dg w_gate + du w_up,   dw_gate = dg^T x,   dw_up = du^T x     (sums in fp32, rounded once)
  *
  *   dh_dev                  M x F, pitch h_ld          gate_dev, up_dev  as rtoss_gated_ff kept them

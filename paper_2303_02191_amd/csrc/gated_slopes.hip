@@ -19,8 +19,9 @@ template <typename T, int ACT> __device__ __forceinline__ void slopes(float g, f
         dg = dh * u;
         du = dh * g;
     } else if constexpr (ACT == 1) {
-        dg = g > 0.f ? dh * u : 0.f;
-        du = g > 0.f ? dh * g : 0.f;
+        // (products by 0 and a NaN kept, as the formula has it: what is not finite in dh, u or g stays visible)
+        dg = dh * u * (g > 0.f ? 1.f : g <= 0.f ? 0.f : g);
+        du = dh * (g < 0.f ? 0.f : g);
     } else {
         const float s = __builtin_amdgcn_rcpf(1.f + __expf(-g));
         dg = dh * u * (s * (1.f + g * (1.f - s)));
