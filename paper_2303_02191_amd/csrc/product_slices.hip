@@ -82,7 +82,8 @@ __device__ __forceinline__ void product_slices(Product p, int work, int tiles_m,
     const int64_t lda = p.lda * EB, ldb = p.ldb * EB, row = (int64_t)p.R * EB;
     const int S1 = (int)(((int64_t)p.R + STAGE - 1) / STAGE), S = FORM == kBackRows ? 2 * S1 : S1;
     const int rest = p.R - (S1 - 1) * STAGE;  // rows of the sum in the last stage
-    const int begin = (PARTS ? (int)((int64_t)S * part / sum_parts.parts) : 0) + (EACH ? 0 : wave), end = PARTS ? (int)((int64_t)S * (part + 1) / sum_parts.parts) : S;
+    const int begin = (PARTS ? (int)((int64_t)S * part / sum_parts.parts) : 0) + (EACH ? 0 : wave);
+    const int end = PARTS ? (int)((int64_t)S * (part + 1) / sum_parts.parts) : S;
     auto whole = [](int64_t bytes) { return (bytes + 15) & ~(int64_t)15; };  // (dg and du, whose rows are padded)
     auto rows_from = [&](const void* base, int64_t ld, int64_t first, int64_t rows) {
         return Source{(const char*)base + first * ld, (rows - 1 - first) * ld + whole(row)};
@@ -172,7 +173,8 @@ __device__ __forceinline__ void product_slices(Product p, int work, int tiles_m,
     const Output first_out(p, min(channel_of(first_unit, 0), p.N - 1));  // (across: it holds nothing but the place)
     const float first_scale = scale_of(first_unit);
 
-    auto read_and_multiply = [&](const char* base, int s, auto&& then) {
+    // to `sum`; `plain`: fp32 by the fp32 instruction
+    auto read_and_multiply = [&](const char* base, int s, Acc (&sum)[MT][NT], auto plain, auto&& then) {
         u32x4 af[2][MT], bf[2][NT];
         auto read_step = [&](int step) {
 #pragma unroll
@@ -190,7 +192,7 @@ __device__ __forceinline__ void product_slices(Product p, int work, int tiles_m,
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int i = 0; i < MT; ++i) acc[i][n] = Mma16<T>::mma(bf[step][n], af[step][i], acc[i][n]);
+                for (int i = 0; i < MT; ++i) sum[i][n] = Mma16<T>::mma(bf[step][n], af[step][i], sum[i][n]);
         };
         if constexpr (ROWS != kWhole && EB < 4) {  // (the next stage is in registers too: one step at a time)
 #pragma unroll
@@ -214,7 +216,16 @@ __device__ __forceinline__ void product_slices(Product p, int work, int tiles_m,
                 for (int t = 0; t < NT; ++t) keep_first<T>(bf[step][t], valid);
             }
         }
-        if constexpr (sizeof(T) == 4) {
+        if constexpr (decltype(plain)::value) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)  // (of four products, one of each q; the first 16 of the stage)
+#pragma unroll
+                for (int i = 0; i < MT; ++i)
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+                        sum[i][n] = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(float, (uint32_t)bf[0][n][k]),
+                                                                         __builtin_bit_cast(float, (uint32_t)af[0][i][k]), sum[i][n], 0, 0, 0);
+        } else if constexpr (sizeof(T) == 4) {
             // six products of bf16 parts (fp32_split.h), smallest first, all into one accumulator (more would not fit the registers beside another
             // stage).  2-norm of the gated block's error, K = 16, 512, 2048 and a wave for each tile: 0.7, 4.8, 9.9e-7, of library products in
             // fp32 1.1, 5.7, 11.5e-7; of sums split over eight waves, K = 1024, 2.3e-7 and 8.1e-7.
@@ -226,7 +237,7 @@ __device__ __forceinline__ void product_slices(Product p, int work, int tiles_m,
                 const Split8 as = split8(af[0][i], af[1][i]);
                 split_steps<kSplitSix>([&](auto k) {
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) split_step<decltype(k)::value>(bs[n], as, acc[i][n], acc[i][n]);
+                    for (int n = 0; n < NT; ++n) split_step<decltype(k)::value>(bs[n], as, sum[i][n], sum[i][n]);
                 });
             }
         } else {
@@ -234,24 +245,49 @@ __device__ __forceinline__ void product_slices(Product p, int work, int tiles_m,
             multiply_step(1);
         }
     };
+    // fp32 sums of fewer than eight products take the fp32 instruction: what the six parts leave out is more than its roundings there.  2-norm of the
+    // error and the largest in 2^-24 of the sum of magnitudes, K = 1, 2, 4, 8, 32:
+    //     fp32 instruction  2.5e-8 (1.0)  3.1e-8 (1.9)  4.0e-8 (2.9)  5.4e-8 (3.8)  10.2e-8 (4.6)
+    //     six parts         4.0e-8 (4.3)  4.0e-8 (4.4)  3.8e-8 (3.8)  4.0e-8 (3.0)   4.4e-8 (2.1)
+    // Time: the same, but 43 us for 40 where every tile is one such sum (gradients of 2 rows, 990 -> 7682).
+    const bool few = sizeof(T) == 4 && p.R * (FORM == kBackRows ? 2 : 1) < 8;  // uniform
+    const int from = few ? end : begin;
+    constexpr std::integral_constant<bool, sizeof(T) == 4> plain;
+    auto by_fp32 = [&](auto&& run) {
+        if constexpr (decltype(plain)::value)
+            if (few) run(acc);
+    };
     if constexpr (ROWS == kWhole) {
         auto issue = [&](int s) {
             const From f = source(s);
             static_for<PIECES>([&](auto k) { copy(f, lds0, k); });
         };
-        if (begin < end) issue(begin);
-        for (int s = begin; s < end; s += STEP) {
+        auto landed = [] {
             fence();
             __builtin_amdgcn_s_waitcnt(0x0f70);  // the stage has landed
             fence();
-            read_and_multiply(own, s, [&] {
-                fence();
-                __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): its place is free
-                fence();
+        };
+        auto read = [] {
+            fence();
+            __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): its place is free
+            fence();
+        };
+        if (from < end) issue(from);
+        for (int s = from; s < end; s += STEP) {
+            landed();
+            read_and_multiply(own, s, acc, std::false_type{}, [&] {
+                read();
                 if (s + STEP < end) issue(s + STEP);
                 __builtin_amdgcn_sched_barrier(0);
             });
         }
+        by_fp32([&](auto& sum) {
+            for (int s = begin; s < end; s += STEP) {
+                issue(s);
+                landed();
+                read_and_multiply(own, s, sum, plain, read);
+            }
+        });
     } else {
         // ---- through registers: a stage is loaded while the one before is multiplied.  (One wave's LDS instructions run in their order.) ----
         constexpr int PA = A_ACROSS ? AcrossA::kPieces : 8, PB = B_ACROSS ? AcrossB::kPieces : 8;
@@ -276,15 +312,26 @@ __device__ __forceinline__ void product_slices(Product p, int work, int tiles_m,
             }
         };
         const Place place{own, lane};
-        StageInRegisters<T, FORM, ROWS, PIECES, A_COPIES, PA, PB, Place> in_registers(p, place, m0, n0, S1, lane);
-        if (begin < end) in_registers.load(begin);
-        for (int s = begin; s < end; s += STEP) {
+        typedef StageInRegisters<T, FORM, ROWS, PIECES, A_COPIES, PA, PB, Place> Stage;
+        Stage in_registers(p, place, m0, n0, S1, lane);
+        if (from < end) in_registers.load(from);
+        for (int s = from; s < end; s += STEP) {
             in_registers.store(s);
             if (s + STEP < end) in_registers.load(s + STEP);
             fence();
-            read_and_multiply(own, s, [&] {});
+            read_and_multiply(own, s, acc, std::false_type{}, [&] {});
             fence();
         }
+        by_fp32([&](auto& sum) {
+            Stage stage(p, place, m0, n0, S1, Stage::unknown(lane));  // (what it holds is not kept through the loop above)
+            for (int s = begin; s < end; s += STEP) {
+                stage.load(s);
+                stage.store(s);
+                fence();
+                read_and_multiply(own, s, sum, plain, [&] {});
+                fence();
+            }
+        });
     }
 
     struct Sum {

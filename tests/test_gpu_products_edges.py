@@ -60,8 +60,8 @@ def all_pairs(g, u, dh, t):
 @pytest.mark.parametrize("a", [0, 1, 2])
 @pytest.mark.parametrize("dt", list(DT))
 def test_gradients_keep_nan_and_infinities(dt, a):
-    """One row and x = 1: the gradients of the weights are dg and du.  dg = dh u act'(g) and du = dh act(g) in IEEE arithmetic, the slope of a NaN a NaN
-    (fp32: infinite dg and du are operands, and make NaN).  Whole numbers, so that nothing is rounded; with SiLU only what is not finite is compared."""
+    """One row and x = 1: the gradients of the weights are dg and du.  dg = dh u act'(g) and du = dh act(g) in IEEE arithmetic, the slope of a NaN a NaN.
+    Whole numbers, so that nothing is rounded; with SiLU only what is not finite is compared."""
     inf, nan = float("inf"), float("nan")
     t = DT[dt]
     gate, up, dh = all_pairs([nan, 1.0, 2.0, -1.0, 0.0] + ([inf, -inf] if a < 2 else []), [1.0, -2.0, 0.0, inf, nan], [1.0, -2.0, 0.0, inf, -inf, nan], t)
@@ -78,9 +78,55 @@ def test_gradients_keep_nan_and_infinities(dt, a):
     dg, du = (H * V * slope).t(), (H * act).t()
     dx, dwg, dwu = pl.gated_ff_backward(dh, x, w, w, gate, up, act=a)
     for got, want, what in ((dwg, dg, "dw_gate"), (dwu, du, "dw_up")):
-        if dt == "f32":
-            want = torch.where(want.isinf(), nan, want)
         if a == 2:
             got, want = torch.where(got.isfinite(), 0.0, got), torch.where(want.isfinite(), 0.0, want)
         same(got, want.to(t), what)
     assert dx.isnan().all()  # (NaN enters the row's sum)
+
+
+# ---------------------------------------------------------------------------------------------------------
+# short sums in fp32
+# ---------------------------------------------------------------------------------------------------------
+def short_sum_tolerance(n, size):
+    """What fp32 arithmetic keeps to: n products and n - 1 additions, a rounding each, so n half steps of the sum of magnitudes.  Of bf16 parts (h of the
+    first 8 bits, what is left m below 2^-7, l below 2^-16 of the value) the roundings of the sums that m enters come on top, 2^-7 and 2^-6 half steps
+    each, and the dropped l l, 2^-8: below 2^-4 for each product."""
+    return n * U * (1 + 2.0 ** -4) * size
+
+
+@pytest.mark.parametrize("n", [1, 2, 3, 5, 7, 8, 16, 32])
+@pytest.mark.parametrize("pitch", [0, 3])
+def test_gated_ff_f32_short_sums(n, pitch):
+    g = gen(100 + n)
+    M, F = 200, 700
+    x, wg, wu = (normal(g, (rows, n + pitch))[:, :n] for rows in (M, F, F))
+    _, gate, up = pl.gated_ff(x, wg, wu, keep=True)
+    X = x.double()
+    for got, w, what in ((gate, wg.double(), "gate"), (up, wu.double(), "up")):
+        check(got, X @ w.t(), short_sum_tolerance(n, X.abs() @ w.abs().t()), what)
+
+
+@pytest.mark.parametrize("n", [1, 2, 3, 5, 7, 8, 16, 32])
+@pytest.mark.parametrize("K,F", [(120, 300), (36, 2000), (1030, 2100)])
+def test_gradients_f32_of_few_rows(n, K, F):
+    """dg = dh u and du = dh g, rounded once, are the operands; sums of n products (weights)."""
+    g = gen(200 + n + K)
+    x, wg, wu = normal(g, (n, K)), normal(g, (F, K)), normal(g, (F, K))
+    gate, up, dh = (normal(g, (n, F)) for _ in range(3))
+    _, dwg, dwu = pl.gated_ff_backward(dh, x, wg, wu, gate, up, act=0)
+    X = x.double()
+    for got, d, what in ((dwg, (dh * up).double(), "dw_gate"), (dwu, (dh * gate).double(), "dw_up")):
+        check(got, d.t() @ X, short_sum_tolerance(n, d.abs().t() @ X.abs()), what)
+
+
+@pytest.mark.parametrize("F", [1, 2, 3, 4, 8])
+@pytest.mark.parametrize("M,K", [(70, 200), (3000, 260)])
+def test_gradients_f32_of_few_channels(M, K, F):
+    """The gradient of the rows: sums of 2 F products."""
+    g = gen(300 + F + M)
+    x, wg, wu = normal(g, (M, K)), normal(g, (F, K)), normal(g, (F, K))
+    gate, up, dh = (normal(g, (M, F)) for _ in range(3))
+    dx, _, _ = pl.gated_ff_backward(dh, x, wg, wu, gate, up, act=0)
+    dg, du = (dh * up).double(), (dh * gate).double()
+    size = dg.abs() @ wg.double().abs() + du.abs() @ wu.double().abs()
+    check(dx, dg @ wg.double() + du @ wu.double(), short_sum_tolerance(2 * F, size), "dx")
