@@ -359,8 +359,8 @@ rtoss_status rtoss_conv2d_pattern_coherent(const rtoss_wdesc* desc, const rtoss_
  *   - Results may not overlap operands or each other (checked for plain matrices).
  *   - Determinism: as above; one order of additions for a shape, a type, the operands' alignment and pitches and the number
  *     of the device's CUs.
- *   - Sums of 8 and more products of 32-bit floats are formed of bf16 parts, to 32-bit precision; an infinite operand makes the
- *     sums that it enters NaN.  In shorter ones, and of the 16-bit types, it makes them what the type's arithmetic does.
+ *   - Sums of 8 and more products of 32-bit floats are formed of bf16 parts, to 32-bit precision.  What an infinite operand or a
+ *     NaN makes of a sum is what IEEE arithmetic does, in every type; no other result changes with it.
  */
 
 /*

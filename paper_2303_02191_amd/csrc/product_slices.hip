@@ -218,13 +218,17 @@ __device__ __forceinline__ void product_slices(Product p, int work, int tiles_m,
         }
         if constexpr (decltype(plain)::value) {
 #pragma unroll
-            for (int k = 0; k < 4; ++k)  // (of four products, one of each q; the first 16 of the stage)
+            for (int step = 0; step < 2; ++step) {  // of 16 products, four instructions of one of each q
+                if (step && rest <= 16 && S1 == 1) break;  // uniform
 #pragma unroll
-                for (int i = 0; i < MT; ++i)
+                for (int e = 0; e < 4; ++e)
 #pragma unroll
-                    for (int n = 0; n < NT; ++n)
-                        sum[i][n] = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(float, (uint32_t)bf[0][n][k]),
-                                                                         __builtin_bit_cast(float, (uint32_t)af[0][i][k]), sum[i][n], 0, 0, 0);
+                    for (int i = 0; i < MT; ++i)
+#pragma unroll
+                        for (int n = 0; n < NT; ++n)
+                            sum[i][n] = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(float, (uint32_t)bf[step][n][e]),
+                                                                             __builtin_bit_cast(float, (uint32_t)af[step][i][e]), sum[i][n], 0, 0, 0);
+            }
         } else if constexpr (sizeof(T) == 4) {
             // six products of bf16 parts (fp32_split.h), smallest first, all into one accumulator (more would not fit the registers beside another
             // stage).  2-norm of the gated block's error, K = 16, 512, 2048 and a wave for each tile: 0.7, 4.8, 9.9e-7, of library products in
@@ -250,12 +254,28 @@ __device__ __forceinline__ void product_slices(Product p, int work, int tiles_m,
     //     fp32 instruction  2.5e-8 (1.0)  3.1e-8 (1.9)  4.0e-8 (2.9)  5.4e-8 (3.8)  10.2e-8 (4.6)
     //     six parts         4.0e-8 (4.3)  4.0e-8 (4.4)  3.8e-8 (3.8)  4.0e-8 (3.0)   4.4e-8 (2.1)
     // Time: the same, but 43 us for 40 where every tile is one such sum (gradients of 2 rows, 990 -> 7682).
+    // And a wave's sums are formed once more so if there is a NaN among them: an infinite operand's parts make a NaN of what may be infinite.  The NaN alone
+    // are replaced, so that a result does not depend on other rows and channels.  Looking for them takes 0 to 4 % (all 0.4 us of 11 where a sum is one
+    // stage); with a NaN in every tile 8192, 512 rows x 1024 -> 2752 take 1380, 97 us for 655, 45.
     const bool few = sizeof(T) == 4 && p.R * (FORM == kBackRows ? 2 : 1) < 8;  // uniform
     const int from = few ? end : begin;
     constexpr std::integral_constant<bool, sizeof(T) == 4> plain;
     auto by_fp32 = [&](auto&& run) {
-        if constexpr (decltype(plain)::value)
-            if (few) run(acc);
+        if constexpr (decltype(plain)::value) {
+            Acc all = {0, 0, 0, 0};  // NaN where one of its terms is (infinities of both signs: looked for in vain)
+#pragma unroll
+            for (int i = 0; i < MT * NT; ++i) all += acc[i / NT][i % NT];
+            if (__builtin_expect(!few && __ballot(__builtin_isnan(all[0] + all[1] + all[2] + all[3])) == 0, 1)) return;
+            Acc sum[MT][NT];
+#pragma unroll
+            for (int i = 0; i < MT * NT; ++i) sum[i / NT][i % NT] = Acc{0, 0, 0, 0};
+            run(sum);
+#pragma unroll
+            for (int i = 0; i < MT * NT * 4; ++i) {
+                const float v = acc[i / 4 / NT][i / 4 % NT][i % 4];
+                acc[i / 4 / NT][i / 4 % NT][i % 4] = few || __builtin_isnan(v) ? sum[i / 4 / NT][i / 4 % NT][i % 4] : v;
+            }
+        }
     };
     if constexpr (ROWS == kWhole) {
         auto issue = [&](int s) {
@@ -323,7 +343,9 @@ __device__ __forceinline__ void product_slices(Product p, int work, int tiles_m,
             fence();
         }
         by_fp32([&](auto& sum) {
-            Stage stage(p, place, m0, n0, S1, Stage::unknown(lane));  // (what it holds is not kept through the loop above)
+            // (nothing of it is kept through the loop above.  Without offsets of whole stages the gated block spills less there, 2048 x 333 -> 2801 122 us
+            // with and 108 without; the gradients more, 512 x 1023 -> 2751 127 and 136)
+            Stage stage(p, place, m0, n0, S1, Stage::unknown(lane), !GATED);
             for (int s = begin; s < end; s += STEP) {
                 stage.load(s);
                 stage.store(s);

@@ -29,7 +29,7 @@ template <typename T, int FORM, int ROWS, int COUNT, int A_COUNT, int PA, int PB
     const int64_t lda = p.lda * EB, ldb = p.ldb * EB;
     // Where all pieces of a stage can be loaded whole, offsets from the tile that do not change, on a uniform base.  (Of rows further apart every
     // piece is found by itself.)
-    const bool near = lda <= 1 << 24 && ldb <= 1 << 24;
+    const bool near;
     uint32_t at_piece[COUNT], at_end[KEPT];
     u32x4 piece_in[COUNT];
     uint32_t end_in[KEPT];
@@ -71,8 +71,8 @@ template <typename T, int FORM, int ROWS, int COUNT, int A_COUNT, int PA, int PB
     }
     static __device__ __forceinline__ int end_of(int j, int lane) { return min(8 * j + (lane & 7), COUNT - 1); }  // whose row's end a lane loads
 
-    __device__ __forceinline__ StageInRegisters(const Product& p, const Place& place, int64_t m0, int n0, int S1, int lane)
-        : p(p), place(place), m0(m0), n0(n0), S1(S1), lane(lane)
+    __device__ __forceinline__ StageInRegisters(const Product& p, const Place& place, int64_t m0, int n0, int S1, int lane, bool whole_stages = true)
+        : p(p), place(place), m0(m0), n0(n0), S1(S1), lane(lane), near(whole_stages && lda <= 1 << 24 && ldb <= 1 << 24)
     {
 #pragma unroll
         for (int i = 0; i < COUNT; ++i) at_piece[i] = near_row(i, lane) + near_piece(i, lane % pieces(i));

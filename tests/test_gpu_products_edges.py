@@ -84,6 +84,65 @@ def test_gradients_keep_nan_and_infinities(dt, a):
     assert dx.isnan().all()  # (NaN enters the row's sum)
 
 
+def same_where_not_finite(got, want, what):
+    t = got.dtype
+    same(torch.where(got.isfinite(), 0.0, got.float()), torch.where(want.isfinite(), 0.0, want).float(), what)
+    assert got.dtype == t
+
+
+# slices of every width, a tile for every wave (fp32), tiles (16 bits); K from below a stage to several
+SPOILT = [(40, 96, 130), (10, 9, 20), (33, 1030, 96), (300, 520, 387), (1500, 16, 2801), (600, 256, 520), (1030, 640, 2100)]
+
+
+@pytest.mark.parametrize("pitch", [0, 3])
+@pytest.mark.parametrize("dt", list(DT))
+@pytest.mark.parametrize("M,K,F", SPOILT)
+def test_gated_ff_of_operands_that_are_not_finite(M, K, F, dt, pitch):
+    """A sum with an infinite operand is infinite, of both signs or with a NaN a NaN, in every type; all others have the bits that they have without."""
+    g = gen(500 + M + pitch)
+    t = DT[dt]
+    inf, nan = float("inf"), float("nan")
+    x, wg, wu = (normal(g, (rows, K + pitch)).to(t)[:, :K] for rows in (M, F, F))
+    clean = pl.gated_ff(x, wg, wu, act=1, keep=True)
+    x[2, 5], x[7, 0], x[8, 3], x[8, K - 1], x[9, K - 1] = inf, -inf, inf, -inf, nan
+    wg[4, 1] = inf
+    h, gate, up = pl.gated_ff(x, wg, wu, act=1, keep=True)
+    G, V = (x.double().cpu() @ w.double().cpu().t() for w in (wg, wu))
+    for got, want, what in ((gate, G, "gate"), (up, V, "up"), (h, torch.relu(G) * V, "h")):
+        same_where_not_finite(got.cpu(), want, what)
+    rows = [m for m in range(M) if m not in (2, 7, 8, 9)]
+    cols = [f for f in range(F) if f != 4]
+    for got, want, what in zip((h, gate, up), clean, ("h", "gate", "up")):
+        equal(got[rows][:, cols], want[rows][:, cols], what)
+
+
+@pytest.mark.parametrize("pitch", [0, 3])
+@pytest.mark.parametrize("dt", list(DT))
+@pytest.mark.parametrize("M,K,F", SPOILT + [(20, 70, 3333), (4100, 33, 20)])
+def test_gradients_of_operands_that_are_not_finite(M, K, F, dt, pitch):
+    """The same of the gradients (dg = dh u, du = dh g)."""
+    g = gen(600 + M + pitch)
+    t = DT[dt]
+    inf, nan = float("inf"), float("nan")
+    x, wg, wu = (normal(g, (rows, K + pitch)).to(t)[:, :K] for rows in (M, F, F))
+    gate, up = normal(g, (M, F)).to(t), normal(g, (M, F)).to(t)
+    dh = normal(g, (M, F + pitch)).to(t)[:, :F]
+    clean = pl.gated_ff_backward(dh, x, wg, wu, gate, up, act=0)
+    dh[2, 3], dh[5, F - 1], dh[6, 0], dh[6, 7] = inf, -inf, nan, inf
+    x[8, 1], wu[4, 2] = inf, -inf
+    got = pl.gated_ff_backward(dh, x, wg, wu, gate, up, act=0)
+    dg, du = (dh.float() * up.float()).to(t).double().cpu(), (dh.float() * gate.float()).to(t).double().cpu()
+    X, G, V = (v.double().cpu() for v in (x, wg, wu))
+    for a, b, what in zip(got, (dg @ G + du @ V, dg.t() @ X, du.t() @ X), ("dx", "dw_gate", "dw_up")):
+        same_where_not_finite(a.cpu(), b, what)
+    rows = [m for m in range(M) if m not in (2, 5, 6)]
+    channels = [f for f in range(F) if f not in (0, 3, 7, F - 1)]
+    cols = [k for k in range(K) if k not in (1, 2)]
+    equal(got[0][rows][:, cols], clean[0][rows][:, cols], "dx")
+    for a, b, what in zip(got[1:], clean[1:], ("dw_gate", "dw_up")):
+        equal(a[channels][:, cols], b[channels][:, cols], what)
+
+
 # ---------------------------------------------------------------------------------------------------------
 # short sums in fp32
 # ---------------------------------------------------------------------------------------------------------
