@@ -1,8 +1,9 @@
 // Gradients of the gated block's two projections from that of its result h = act(g) * u:
 //     dg = dh * u * act'(g),   du = dh * act(g)
-// with s = 1 / (1 + exp(-g)) for SiLU: act = g s, act' = s (1 + g (1 - s)).  fp32; dg and du are rounded once to the operands' type, in
-// which the products behind read them.  (A reciprocal is off by 1 ulp at most, far below that rounding; in fp32 it is one of three
-// roundings of the product.)
+// with s = 1 / (1 + exp(-g)) for SiLU: act = g s, act' = s (1 + g (1 - s)).  In fp32 the quotients are those of the forward pass, to the bit; in 16 bits a
+// reciprocal off by 1 ulp, far below the rounding.
+//
+// dg and du are rounded once to the operands' type, in which the products behind read them.
 //
 // Bound: memory, five tensors of M * F elements.
 #include <algorithm>
@@ -22,6 +23,10 @@ template <typename T, int ACT> __device__ __forceinline__ void slopes(float g, f
         // (products by 0 and a NaN kept, as the formula has it: what is not finite in dh, u or g stays visible)
         dg = dh * u * (g > 0.f ? 1.f : g <= 0.f ? 0.f : g);
         du = dh * (g < 0.f ? 0.f : g);
+    } else if constexpr (sizeof(T) == 4) {
+        const float s = 1.f / (1.f + __expf(-g));
+        dg = dh * u * (s * (1.f + g * (1.f - s)));
+        du = dh * silu_divided(g);
     } else {
         const float s = __builtin_amdgcn_rcpf(1.f + __expf(-g));
         dg = dh * u * (s * (1.f + g * (1.f - s)));

@@ -189,3 +189,17 @@ def test_gradients_f32_of_few_channels(M, K, F):
     dg, du = (dh * up).double(), (dh * gate).double()
     size = dg.abs() @ wg.double().abs() + du.abs() @ wu.double().abs()
     check(dx, dg @ wg.double() + du @ wu.double(), short_sum_tolerance(2 * F, size), "dx")
+
+
+def test_gradients_f32_take_the_activation_of_the_forward_pass():
+    """du = dh act(g) with the act(g) of the forward pass, bit for bit: u = 1 and dh = 1, sums of one product by 1."""
+    g = gen(400)
+    v = torch.cat([normal(g, (3000, 1), 3.0), torch.linspace(-100, 100, 1001, device="cuda")[:, None]])
+    F = v.shape[0]
+    one, zero = torch.ones_like(v), torch.zeros_like(v)
+    x, wg, wu = torch.ones(1, 2, device="cuda"), torch.cat([v, zero], 1), torch.cat([zero, one], 1)
+    h, gate, up = pl.gated_ff(x, wg, wu, keep=True)
+    equal(gate, v.t())
+    equal(up, one.t())
+    _, dwg, dwu = pl.gated_ff_backward(torch.ones(1, F, device="cuda"), x, wg, wu, gate, up)
+    equal(dwu[:, :1], h.t(), "du")
