@@ -356,7 +356,7 @@ rtoss_status rtoss_conv2d_pattern_coherent(const rtoss_wdesc* desc, const rtoss_
  *     Pointers and pitches need only the alignment of their elements; rows of whole 16-byte pieces that start at multiples of
  *     16 bytes are the fast path, rows that start at multiples of 4 the next.
  *   - Rows 0 <= M < 2^31 (M = 0: nothing to do, row pointers may be NULL), channels 1 .. 2^24, pitches below 2^31 elements.
- *   - Results may not overlap operands or each other (checked for plain matrices).
+ *   - Results may not overlap operands, scales or each other (checked, but for two slices of different pitches).
  *   - Determinism: as above; one order of additions for a shape, a type, the operands' alignment and pitches and the number
  *     of the device's CUs.
  *   - Sums of 8 and more products of 32-bit floats are formed of bf16 parts, to 32-bit precision.  What an infinite operand or a

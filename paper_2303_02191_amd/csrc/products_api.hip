@@ -20,15 +20,21 @@ constexpr int64_t kMaxPitch = 0x7fffffff;
 
 // A matrix of rows in memory: where its bytes are.
 struct Span {
-    const char *from, *to;
-    bool plain;  // its rows without gaps (two slices of one wider buffer interleave without sharing an element)
+    int64_t from, rows, width, pitch;  // in bytes, one row of a matrix without gaps
 };
 Span span(const void* p, int64_t rows, int64_t width, int64_t ld, int eb)
 {
-    const char* c = (const char*)p;
-    return Span{c, p && rows > 0 ? c + ((rows - 1) * ld + width) * eb : c, ld == width || rows <= 1};
+    const Span s{(int64_t)(uintptr_t)p, p ? rows : 0, width * eb, ld * eb};
+    return s.rows > 1 && ld == width ? Span{s.from, 1, s.rows * s.width, s.rows * s.width} : s;
 }
-bool overlap(const Span& a, const Span& b) { return a.plain && b.plain && a.from < b.to && b.from < a.to; }
+// Whether rows i of a and j of b share a byte: -b.width < b.from - a.from + j b.pitch - i a.pitch < a.width.  (Of slices with different pitches: not looked for.)
+bool overlap(const Span& a, const Span& b)
+{
+    if (!a.rows || !b.rows || (a.rows > 1 && b.rows > 1 && a.pitch != b.pitch)) return false;
+    const auto below = [](int64_t n, int64_t by) { return n / by - (n % by < 0); };  // rounded down
+    const int64_t pitch = a.rows > 1 ? a.pitch : b.pitch, apart = b.from - a.from;
+    return std::max(below(-b.width - apart, pitch) + 1, 1 - a.rows) <= std::min(below(a.width - apart - 1, pitch), b.rows - 1);  // j - i
+}
 
 rtoss_status check_rows(int64_t M, const char* what)
 {
@@ -372,8 +378,10 @@ rtoss_status rtoss_matmul_i8(const rtoss_matmul_desc* desc, const int8_t* a_dev,
     RTOSS_TRY(check_pointer(y_dev, eb, "y_dev"));
     if (misaligned(e.residual_dev, eb)) return fail(RTOSS_EINVAL, "residual_dev is not aligned to its element size");
     const Span y = span(y_dev, d.M, d.N, y_ld, eb);
-    if (overlap(y, span(a_dev, d.M, d.K, d.a_ld, 1)) || overlap(y, span(w_dev, d.N, d.K, d.w_ld, 1))) return fail(RTOSS_EINVAL, "operands and y overlap");
-    if (overlap(y, span(e.residual_dev, e.residual_dev ? d.M : 0, d.N, residual_ld, eb))) return fail(RTOSS_EINVAL, "residual and y overlap");
+    const Span in[] = {span(a_dev, d.M, d.K, d.a_ld, 1), span(w_dev, d.N, d.K, d.w_ld, 1), span(a_scale_dev, d.M, 1, 1, 4),
+                       span(e.scale_dev, d.N, 1, 1, 4),  span(e.bias_dev, d.N, 1, 1, 4),   span(e.residual_dev, d.M, d.N, residual_ld, eb)};
+    for (const Span& i : in)
+        if (overlap(y, i)) return fail(RTOSS_EINVAL, "operands, scales, bias or residual and y overlap");
     Product p{};
     p.a0 = a_dev;
     p.b0 = w_dev;
@@ -407,7 +415,7 @@ rtoss_status rtoss_gated_ff(const rtoss_gated_desc* desc, const void* x_dev, con
     RTOSS_TRY(check_pointer(h_dev, eb, "h_dev"));
     if (misaligned(gate_dev, eb) || misaligned(up_dev, eb)) return fail(RTOSS_EINVAL, "gate_dev and up_dev are not aligned to their element size");
     const Span in[] = {span(x_dev, d.M, d.K, d.x_ld, eb), span(w_gate_dev, d.F, d.K, d.w_ld, eb), span(w_up_dev, d.F, d.K, d.w_ld, eb)};
-    const Span out[] = {span(h_dev, d.M, d.F, d.h_ld, eb), span(gate_dev, gate_dev ? d.M : 0, d.F, d.F, eb), span(up_dev, up_dev ? d.M : 0, d.F, d.F, eb)};
+    const Span out[] = {span(h_dev, d.M, d.F, d.h_ld, eb), span(gate_dev, d.M, d.F, d.F, eb), span(up_dev, d.M, d.F, d.F, eb)};
     for (const Span& o : out) {
         for (const Span& i : in)
             if (overlap(o, i)) return fail(RTOSS_EINVAL, "operands and results overlap");
@@ -447,8 +455,10 @@ rtoss_status rtoss_gated_ff_i8(const rtoss_gated_desc* desc, const int8_t* a_dev
     RTOSS_TRY(check_pointer(w_up_dev, 1, "w_up_dev"));
     RTOSS_TRY(check_pointer(h_dev, eb, "h_dev"));
     const Span h = span(h_dev, d.M, d.F, d.h_ld, eb);
-    if (overlap(h, span(a_dev, d.M, d.K, d.x_ld, 1)) || overlap(h, span(w_gate_dev, d.F, d.K, d.w_ld, 1)) || overlap(h, span(w_up_dev, d.F, d.K, d.w_ld, 1)))
-        return fail(RTOSS_EINVAL, "operands and h overlap");
+    const Span in[] = {span(a_dev, d.M, d.K, d.x_ld, 1),      span(w_gate_dev, d.F, d.K, d.w_ld, 1), span(w_up_dev, d.F, d.K, d.w_ld, 1),
+                       span(a_scale_dev, d.M, 1, 1, 4),       span(gate_scale_dev, d.F, 1, 1, 4),    span(up_scale_dev, d.F, 1, 1, 4)};
+    for (const Span& i : in)
+        if (overlap(h, i)) return fail(RTOSS_EINVAL, "operands or scales and h overlap");
     Product p{};
     p.a0 = a_dev;
     p.b0 = w_gate_dev;

@@ -203,3 +203,31 @@ def test_gradients_f32_take_the_activation_of_the_forward_pass():
     equal(up, one.t())
     _, dwg, dwu = pl.gated_ff_backward(torch.ones(1, F, device="cuda"), x, wg, wu, gate, up)
     equal(dwu[:, :1], h.t(), "du")
+
+
+# ---------------------------------------------------------------------------------------------------------
+# slices side by side
+# ---------------------------------------------------------------------------------------------------------
+def test_operands_and_results_side_by_side_in_one_buffer():
+    g = gen(450)
+    M, K, N = 37, 48, 40
+    buf = torch.zeros(M, 2 * N + K, device="cuda")
+    res, y, x = buf[:, :N], buf[:, N:2 * N], buf[:, 2 * N:]
+    res.copy_(whole(g, (M, N), 9))
+    x.copy_(whole(g, (M, K), 2))
+    a, w = codes(g, (M, K)), codes(g, (N, K))
+    before = buf.clone()
+    assert pl.matmul_i8(a, None, w, None, residual=res, out_dt=B.F32, y=y) is y
+    equal(y, (a.double() @ w.double().t()).float() + before[:, :N])
+    wg, wu = whole(g, (N, K), 1), whole(g, (N, K), 1)
+    pl.gated_ff(x, wg, wu, act=0, h=y)
+    equal(y, ((x.double() @ wg.double().t()) * (x.double() @ wu.double().t())).float())
+    equal(buf[:, :N], before[:, :N])
+    equal(buf[:, 2 * N:], before[:, 2 * N:])
+    one = torch.zeros(4 * M * K, dtype=torch.uint8, device="cuda")  # every row's codes in a gap of the rows
+    rows = one.view(torch.bfloat16).view(M, 2 * K)
+    q = one.view(torch.int8).view(M, 4 * K)[:, 2 * K:3 * K]
+    rows[:, :K].copy_(x)
+    _, s = pl.quantize_rows(rows[:, :K], q=q)
+    equal(q.float() * s[:, None], q.float() * (x.abs().amax(1) / 127)[:, None])
+    equal(q, torch.where(x.abs().amax(1, keepdim=True) > 0, x * 127 / x.abs().amax(1, keepdim=True), 0.0).double().round().to(torch.int8))
