@@ -423,9 +423,12 @@ rtoss_status rtoss_gated_ff_i8(const rtoss_gated_desc* desc, const int8_t* a_dev
 
 /*
  * Gradients of rtoss_gated_ff from that of h:
- *     dg = dh * u * act'(g),  du = dh * act(g)     (in fp32, then rounded to dt, in whose range they have to lie; act' of ReLU
- *                                                   at 0 is 0, of a NaN a NaN; a zero times an infinity is a NaN here too)
+ *     dg = dh * u * act'(g),  du = dh * act(g)     (act' of ReLU at 0 is 0, of a NaN a NaN; a zero times an infinity is a NaN)
  *     dx = dg w_gate + du w_up,   dw_gate = dg^T x,   dw_up = du^T x     (sums in fp32, rounded once)
+ *
+ * dg and du are formed in fp32 and rounded to dt, as operands of the products: in 16 bits the gradients' error is some 1.4 times that of
+ * their own rounding.  In RTOSS_F16 dg and du have its range: scale dh so that they neither pass 65504 (they are infinite then) nor lie
+ * below 2^-14 (they lose bits).
  *
  *   dh_dev                  M x F, pitch h_ld          gate_dev, up_dev  as rtoss_gated_ff kept them
  *   dx_dev                  out: plain [M][K], or NULL (not computed; the weights may then be NULL)

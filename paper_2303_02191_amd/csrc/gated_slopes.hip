@@ -3,7 +3,10 @@
 // with s = 1 / (1 + exp(-g)) for SiLU: act = g s, act' = s (1 + g (1 - s)).  In fp32 the quotients are those of the forward pass, to the bit; in 16 bits a
 // reciprocal off by 1 ulp, far below the rounding.
 //
-// dg and du are rounded once to the operands' type, in which the products behind read them.
+// dg and du are rounded once to the operands' type, in which the products behind read them: the 2-norm of the gradients' error is sqrt 2 times that of
+// unrounded ones (bf16 2.34e-3 and 1.66e-3, fp16 2.9e-4 and 2.1e-4, of which the gradients' own rounding is the smaller figure).  Held in two parts of 16 bits each
+// they would double the matrix products, 94 % of the time (8192 x 4096, 10944).  So in fp16 they have its range: below 2^-14 they have fewer bits, above
+// 65504 they are infinite.
 //
 // Bound: memory, five tensors of M * F elements.
 #include <algorithm>

@@ -231,3 +231,54 @@ def test_operands_and_results_side_by_side_in_one_buffer():
     _, s = pl.quantize_rows(rows[:, :K], q=q)
     equal(q.float() * s[:, None], q.float() * (x.abs().amax(1) / 127)[:, None])
     equal(q, torch.where(x.abs().amax(1, keepdim=True) > 0, x * 127 / x.abs().amax(1, keepdim=True), 0.0).double().round().to(torch.int8))
+
+
+# ---------------------------------------------------------------------------------------------------------
+# workspaces of gradients whose sums are shared by workgroups, and gradients far from 1
+# ---------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("wanted", [(True, True), (True, False), (False, True)])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("M,K,F", [(20, 70, 3333), (8192, 64, 40), (1500, 60, 1600), (130, 64, 9000)])
+def test_workspaces_of_shared_sums(M, K, F, dt, wanted):
+    """Counters and parts behind dg and du, in memory that holds anything; nothing is written behind the size asked for."""
+    g = gen(460 + M)
+    t = DT[dt]
+    x, wg, wu = whole(g, (M, K), 2, t), whole(g, (F, K), 1, t), whole(g, (F, K), 1, t)
+    gate, up, dh = (whole(g, (M, F), 2, t) for _ in range(3))
+    n = B.rtoss_gated_ff_backward_size(B.GatedDesc(M, K, F, {"f32": B.F32, "bf16": B.BF16}[dt], B.ACT_NONE, 0, 0, 0))
+    pitch = -(-F // (16 // t.itemsize)) * 16  # bytes
+    assert n > 2 * (-(-M * pitch // 256) * 256), "this shape shares no sums"
+    dg, du = dh.double() * up.double(), dh.double() * gate.double()
+    want = [(dg @ wg.double() + du @ wu.double()).to(t), (dg.t() @ x.double()).to(t), (du.t() @ x.double()).to(t)]
+    space = torch.empty(n + (1 << 20), dtype=torch.uint8, device="cuda")
+    for fill in (201, 0, 255):
+        space.fill_(fill)
+        space[n:] = 77
+        got = pl.gated_ff_backward(dh, x, wg, wu, gate, up, act=0, rows=wanted[0], weights=wanted[1], workspace=space[:n])
+        assert (space[n:] == 77).all()
+        for a, b, asked in zip(got, want, (wanted[0], wanted[1], wanted[1])):
+            assert (a is not None) == asked
+            if asked:
+                equal(a, b, "fill %d" % fill)
+
+
+@pytest.mark.parametrize("scale", [2.0 ** -20, 2.0 ** -12, 2.0 ** 8])
+def test_gradients_f16_far_from_one(scale):
+    """dh at other scales: dg and du are rounded to fp16, among its subnormal numbers too, half a step each."""
+    g = gen(470)
+    t = torch.float16
+    M, K, F = 70, 96, 130
+    x, wg, wu = normal(g, (M, K)).to(t), normal(g, (F, K), K ** -0.5).to(t), normal(g, (F, K), K ** -0.5).to(t)
+    gate, up, dh = normal(g, (M, F)).to(t), normal(g, (M, F)).to(t), (normal(g, (M, F)) * scale).to(t)
+    dx, dwg, dwu = pl.gated_ff_backward(dh, x, wg, wu, gate, up, act=0)
+    dg, du = dh.double() * up.double(), dh.double() * gate.double()
+    eg, eu = ((half_step(t) + U) * v.abs() + least(t) for v in (dg, du))
+    X, W, V = x.double(), wg.double(), wu.double()
+
+    def close(got, want, error, size, n, what):
+        tol = error + 2 * (n + 4) * U * size
+        check(got, want, tol + half_step(t) * (want.abs() + tol) + least(t), what)
+
+    close(dx, dg @ W + du @ V, eg @ W.abs() + eu @ V.abs(), (dg.abs() + eg) @ W.abs() + (du.abs() + eu) @ V.abs(), 2 * F, "dx")
+    close(dwg, dg.t() @ X, eg.t() @ X.abs(), (dg.abs() + eg).t() @ X.abs(), M, "dw_gate")
+    close(dwu, du.t() @ X, eu.t() @ X.abs(), (du.abs() + eu).t() @ X.abs(), M, "dw_up")
