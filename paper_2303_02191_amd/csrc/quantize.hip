@@ -151,8 +151,8 @@ template <typename T> rtoss_status launch_lanes(const void* x_, int64_t M, int K
 {
     const T* x = (const T*)x_;
     const int vectors = (int)(((int64_t)K * (int)sizeof(T) + 15) / 16);
+    if (vectors <= 16) return launch<T, 16, 1>(x, M, K, ldx, q, ldq, scale, s);
 #define RTOSS_LANES(LANES)                                                                     \
-    if (vectors <= LANES) return launch<T, LANES, 1>(x, M, K, ldx, q, ldq, scale, s);          \
     if (vectors <= 2 * LANES) return launch<T, LANES, 2>(x, M, K, ldx, q, ldq, scale, s);      \
     if (vectors <= 4 * LANES) return launch<T, LANES, 4>(x, M, K, ldx, q, ldq, scale, s)
     RTOSS_LANES(16);
