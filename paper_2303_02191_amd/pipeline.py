@@ -69,7 +69,8 @@ def reduce_dictionary(masks, w_random, dt, M):
 
 
 # Rows are the positions (tokens) of a tensor whose last dimension is the channels; they may lie in a wider buffer.  Results are allocated
-# unless they are given.  Calls run on the tensors' GPU, on its current stream.
+# unless they are given.  Calls run on the tensors' GPU, on its current stream.  Nothing is recorded for torch's autograd, as nowhere here: a result has no
+# history whatever its inputs require, and gated_ff_backward is called for the gradients.
 def quantize_rows(x, q=None, scale=None):
     """Signed 8-bit codes and a scale for each row of x [..., K] (float32, float16 or bfloat16): activations by token, weights [N, K] by
     output channel.  Returns (q [..., K] int8, scale [...] float32)."""
@@ -84,7 +85,7 @@ def matmul_i8(a, a_scale, w, w_scale, bias=None, act=B.ACT_NONE, residual=None, 
 
 def gated_ff(x, w_gate, w_up, act=B.ACT_SILU, keep=False, h=None):
     """h = act(x w_gate^T) * (x w_up^T).  x: rows [..., K]; weights [F, K] of x's dtype.  Returns h [..., F]; with keep, (h, gate, up): the two
-    projections, which gated_ff_backward takes."""
+    projections, which gated_ff_backward takes (autograd sees none of it)."""
     return B.host().gated_ff(x, w_gate, w_up, act, keep, h)
 
 

@@ -282,3 +282,45 @@ def test_gradients_f16_far_from_one(scale):
     close(dx, dg @ W + du @ V, eg @ W.abs() + eu @ V.abs(), (dg.abs() + eg) @ W.abs() + (du.abs() + eu) @ V.abs(), 2 * F, "dx")
     close(dwg, dg.t() @ X, eg.t() @ X.abs(), (dg.abs() + eg).t() @ X.abs(), M, "dw_gate")
     close(dwu, du.t() @ X, eu.t() @ X.abs(), (du.abs() + eu).t() @ X.abs(), M, "dw_up")
+
+
+# ---------------------------------------------------------------------------------------------------------
+# shapes of tensors
+# ---------------------------------------------------------------------------------------------------------
+def test_one_row_as_a_vector_and_channels_of_one():
+    g = gen(480)
+    K, F = 72, 50
+    x, wg, wu, dh = whole(g, (K,), 2), whole(g, (F, K), 1), whole(g, (F, K), 1), whole(g, (F,), 2)
+    q, s = pl.quantize_rows(x)
+    assert q.shape == (K,) and s.shape == ()
+    equal(q, (x.double() * 127 / x.abs().max()).round().to(torch.int8))
+    y = pl.matmul_i8(q, s, codes(gen(1), (F, K)), None, out_dt=B.F32)
+    equal(y, (q.double() @ codes(gen(1), (F, K)).double().t()).float() * s)
+    h, gate, up = pl.gated_ff(x, wg, wu, act=1, keep=True)
+    assert h.shape == gate.shape == up.shape == (F,)
+    G, V = wg.double() @ x.double(), wu.double() @ x.double()
+    equal(h, (torch.relu(G) * V).float())
+    dx, dwg, dwu = pl.gated_ff_backward(dh, x, wg, wu, gate, up, act=0)
+    dg, du = dh.double() * V, dh.double() * G
+    equal(dx, (dg @ wg.double() + du @ wu.double()).float())
+    equal(dwg, (dg[:, None] * x.double()).float())
+    equal(dwu, (du[:, None] * x.double()).float())
+    column = whole(g, (1, 40), 2).t()  # [40, 1] of rows one element apart, its last stride 40
+    w = whole(g, (F, 1), 2)
+    equal(pl.gated_ff(column, w, w, act=0), (column.double() * w[:, 0].double()).square().float())
+    one = torch.zeros(3, 1, 5, K, device="cuda")[:, :, ::2]  # rows 2 K apart within a block, the blocks 5 K: no constant pitch
+    with pytest.raises(AssertionError, match="distance"):
+        pl.quantize_rows(one)
+
+
+def test_workspaces_that_do_not_fit_are_refused():
+    g = gen(481)
+    x, w, t = whole(g, (20, 70), 2), whole(g, (3333, 70), 1), whole(g, (20, 3333), 2)
+    n = B.rtoss_gated_ff_backward_size(B.GatedDesc(20, 70, 3333, B.F32, B.ACT_NONE, 0, 0, 0))
+    space = torch.empty(n + 512, dtype=torch.uint8, device="cuda")
+    for bad in (space[:n - 1], space[128:128 + n]):
+        with pytest.raises(B.RtossError, match="workspace"):
+            pl.gated_ff_backward(t, x, w, w, t, t, act=0, workspace=bad)
+    for bad in (space[:n].view(torch.int8), torch.empty(2 * n, dtype=torch.uint8, device="cuda")[::2]):
+        with pytest.raises(AssertionError, match="workspace"):
+            pl.gated_ff_backward(t, x, w, w, t, t, act=0, workspace=bad)
