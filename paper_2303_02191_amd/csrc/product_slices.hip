@@ -10,7 +10,7 @@
 //   - Of many tiles with short sums, and of fp32 in general, every wave has one of its own, and nothing is joined.
 // Bound: weights' bytes where there are few rows (bf16 1 x 4096 -> 10944 twice 34 us, 5.2 TB/s; 8-bit 1 x 4096 x 4096 5.2 us, of which a launch
 // is 3), otherwise the copies, 64 bytes a cycle and CU (8-bit 256 x 4096 x 4096 10 us); fp32: the splitting and six bf16 products (1024 ->
-// 2752 of 512, 2048, 8192 rows 42, 151, 531 us, 138 to 174 TFLOP/s; a library product of 8192^3 153).
+// 2752 of 512, 2048, 8192 rows, nothing kept, 45 to 53, 171, 543 us, 110 to 170 TFLOP/s; a library product of 8192^3 153).
 #include <algorithm>
 
 #include "fp32_split.h"
