@@ -81,8 +81,9 @@ rtoss_status gated_desc(const rtoss_gated_desc* desc, rtoss_gated_desc* d)
 }
 
 // The kernel for a product: the one whose estimate is shortest.  All are bound by what a CU can copy in the small, by the matrix instructions
-// in the large, and by whole rounds of workgroups.  Constants in us, for 256 CUs, fitted to 456 products of the forward pass in all tiles (the choice
-// is 1.2 % longer than the best in the mean, 25 % at most); rows of whole 16-byte pieces, of words, of bytes:
+// in the large, and by whole rounds of workgroups.  Constants in us, for 256 CUs, fitted to 456 products of the forward pass in all tiles (measured again on
+// 111 of such with the kernels as they are, the choice is 2.0 % longer than the best in the mean, 31 % at most); rows of whole 16-byte pieces, of words, of
+// bytes:
 //   slices of a x b: the launch 3.1, then for each round a little more the larger the tile, and the rows of both operands at 72, 41, 37 KB/us and CU
 //     (fp32 also 0.77e6 products), or where the sum is short a workgroup's beginning and end.  8-bit 4096 x 4096, rows 1, 64, 128, 256: 5.2, 6.7,
 //     7.6, 9.9 with the tile that this takes; 8.4, 9.4, 9.4, 9.9 with 64 x 64 for all.
